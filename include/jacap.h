@@ -326,9 +326,145 @@ jacap_status jacap_greedy(const jacap_config* cfg, const jacap_batch* batch, con
                           const void* k, const void* v, int32_t* idx, int32_t* order,
                           double* logdet, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Attention over the cache, and eviction by accumulated attention weight.
+ *
+ * jacap_attend is the attention of a decoding step: the S = cfg->window query
+ * rows of every query head are one new token (S = 1) or a tree of drafted
+ * tokens, whose own keys and values are not in the cache yet. With
+ * z_ri = scale q_r . k_i over the cached tokens i of the row's unit and
+ * z_rj = scale q_r . kd_j over the drafted tokens j that row r sees,
+ *
+ *   lse_r = log sum exp(z_r.),   out_r = sum exp(z_r. - lse_r) v.
+ *
+ * A row that sees nothing gives out = 0 and lse = -inf.
+ *
+ * An accumulator holds one float per cached token and KV head, laid out like
+ * the scores: the attention weight the token has received,
+ *
+ *   acc_i <- decay acc_i + sum_r rw_r exp(z_ri - lse_r)
+ *
+ * over the rows r of the G query heads that share the KV head (rw: optional
+ * row weights, else 1). An entry below zero marks an EMPTY SLOT: its token is
+ * hidden from every row whatever its K and V hold (NaN among them), and the
+ * entry stays as it is. jacap_attend adds the weights of its own rows
+ * (attn->accumulate = 1); jacap_attn_weights adds those of a window, of a
+ * whole prompt, or of the accepted rows of a tree whose lse jacap_attend
+ * returned. jacap_evict_weighted and jacap_evict_weighted_slots keep the
+ * budget_k tokens of the largest accumulated weight.
+ *
+ * Lengths: attn->live_lens (optional) holds the sequences' current lengths in
+ * device memory: sequence b owns the rows seq_offsets[b] .. seq_offsets[b+1]-1
+ * of the cache, of which the first live_lens[b] hold tokens (n_b in what
+ * follows); null = all of them. A length below 0 or above the rows raises
+ * JACAP_FLAG_BAD_OFFSETS, as inconsistent offsets do, and the sequence's cache
+ * is taken as empty. Everything these calls read on the device may change
+ * between the replays of a captured graph.
+ *
+ * cfg->temperature, ridge, cov_mode, ridge_mode and gqa_mode are not read for
+ * their meaning here (the entry points check them as everywhere), and budget_k,
+ * protect_last and the batch's out strides only by the eviction calls. Logits,
+ * softmax statistics, sums over tokens and accumulators are fp32; with bf16
+ * inputs the products are exact, the weights that multiply V are rounded to
+ * bf16 (relative 2^-9, as out itself is), and those that are accumulated are
+ * not. NaN and infinite inputs propagate as in the formulas; they raise no
+ * flag. All results are deterministic. */
+typedef struct jacap_attention {
+  float scale;         /* > 0, finite: 1/sqrt(d) for ordinary attention */
+  float decay;         /* 0 .. 1: what an accumulator entry is multiplied by (0: overwritten) */
+  int32_t accumulate;  /* jacap_attend: 1 = add the rows' weights to acc */
+  int32_t causal;      /* jacap_attn_weights: 1 = row p is position n_b - window + p, and sees
+                          the positions up to its own; 0 = every row sees every token */
+  const int32_t* live_lens;  /* device int32 [B], or null */
+  const float* row_weight;   /* device float [B][window], or null; a row of weight 0 adds exactly
+                                nothing, whatever it holds */
+  const uint64_t* tree;      /* jacap_attend: device [B][window][ceil(window / 64)], bit j % 64 of
+                                word j / 64 of a row set where it sees drafted token j (normally
+                                its ancestors and itself); bits at or past window are not read.
+                                null: row s sees the drafted tokens 0 .. s */
+  int64_t dk_stride_seq, dk_stride_layer, dk_stride_head, dk_stride_row; /* drafted keys */
+  int64_t dv_stride_seq, dv_stride_layer, dv_stride_head, dv_stride_row; /* drafted values */
+  int64_t o_stride_seq, o_stride_layer, o_stride_head, o_stride_pos;     /* attention output */
+  int64_t a_stride_seq, a_stride_layer, a_stride_head; /* acc_out of jacap_evict_weighted */
+} jacap_attention;
+
+/* Bytes of workspace of jacap_attend, jacap_attn_weights and
+ * jacap_evict_weighted_slots: upper bounds from the host fields, 256-byte
+ * aligned bases, errors as jacap_workspace_size. */
+jacap_status jacap_attend_workspace_size(const jacap_config* cfg, const jacap_batch* batch,
+                                         const jacap_attention* attn, size_t* bytes);
+jacap_status jacap_attn_weights_workspace_size(const jacap_config* cfg, const jacap_batch* batch,
+                                               const jacap_attention* attn, size_t* bytes);
+jacap_status jacap_evict_weighted_workspace_size(const jacap_config* cfg, const jacap_batch* batch,
+                                                 const jacap_attention* attn, size_t* bytes);
+
+/* Attention of S = cfg->window rows (1 .. 512, else JACAP_ERR_UNSUPPORTED) per
+ * query head over the cache and the drafted tokens.
+ *   q      : [B][L][H_q][S][d], the batch's Q strides, cfg->dtype.
+ *   k, v   : the cache. May be null if total_tokens = 0.
+ *   kd, vd : drafted keys and values [B][L][H_kv][S][d], the dk / dv strides
+ *            (multiples of 8 elements, row strides d .. 2^24).
+ *   out    : [B][L][H_q][S][d], the o strides (multiples of 8), cfg->dtype.
+ *   lse    : optional float [B][L][H_q][S] (dense), natural logarithms.
+ *   acc    : optional float [L][H_kv][T_total] (dense): hides the empty slots,
+ *            and takes the weights when attn->accumulate = 1 (then required
+ *            unless total_tokens = 0). Must not be written by others meanwhile.
+ *   acc_draft : optional float [B][L][H_kv][S] (dense), written only with
+ *            accumulate = 1: the weights the drafted tokens received, what
+ *            their accumulator entries start from when they enter the cache.
+ * The sticky flags (jacap_read_status) hold at most JACAP_FLAG_BAD_OFFSETS. */
+jacap_status jacap_attend(const jacap_config* cfg, const jacap_batch* batch,
+                          const jacap_attention* attn, const void* q, const void* k,
+                          const void* v, const void* kd, const void* vd, void* out, float* lse,
+                          float* acc, float* acc_draft, void* ws, size_t ws_bytes, void* stream);
+
+/* acc_i <- decay acc_i + sum_r rw_r exp(z_ri - lse_r) for every cached token
+ * i < n_b that is not an empty slot, over the cfg->window rows of each query
+ * head (any number). Rows before the sequence's start (attn->causal with
+ * n_b < window) see nothing.
+ *   q       : [B][L][H_q][w][d], the batch's Q strides.
+ *   lse_in  : null = computed here over the tokens each row sees; else float
+ *             [B][L][H_q][w] (dense): the rows' log-sums over all they
+ *             attended to; a row of lse -inf adds nothing.
+ *   lse_out : optional float [B][L][H_q][w] (dense): the computed log-sums
+ *             (-inf for a row that sees nothing). Must be null with lse_in.
+ *   acc     : float [L][H_kv][T_total] (dense), read and written.
+ * V is not read: its strides are checked as everywhere. Flags as jacap_attend. */
+jacap_status jacap_attn_weights(const jacap_config* cfg, const jacap_batch* batch,
+                                const jacap_attention* attn, const void* q, const void* k,
+                                const float* lse_in, float* lse_out, float* acc, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/* Eviction by accumulated weight: jacap_select's rule (weight descending,
+ * position ascending, NaN lowest, cfg->protect_last) on acc over the n_b
+ * tokens of every sequence, then jacap_compact, and the kept tokens'
+ * accumulators with them. Empty slots rank below every token; where fewer than
+ * budget_k tokens are left, they are kept as empty slots.
+ *   idx     : int32 [B][L][H_kv][budget_k], as jacap_select.
+ *   k_out, v_out : as jacap_compact (the batch's out strides).
+ *   acc_out : float, entry j of unit (b, l, h) at b*a_stride_seq +
+ *             l*a_stride_layer + h*a_stride_head + j (any strides >= 0); the
+ *             entries past min(budget_k, n_b) are -1 (empty slots).
+ * attn: live_lens and the a strides are read. No workspace. */
+jacap_status jacap_evict_weighted(const jacap_config* cfg, const jacap_batch* batch,
+                                  const jacap_attention* attn, const float* acc, const void* k,
+                                  const void* v, int32_t* idx, void* k_out, void* v_out,
+                                  float* acc_out, void* stream);
+
+/* The same choice for caches refilled in place (as jacap_select_evicted): the
+ * positions of the n_b - min(budget_k, n_b) evicted tokens, ascending, -1 in
+ * the rest of slots[u][0 .. slot_cap), and acc there set to -1, so that the
+ * slots are empty until the caller writes a token's K, V and weight to them.
+ *   slots : int32 [B][L][H_kv][slot_cap], 16-byte aligned; slot_cap >= max(0,
+ *           max_seq_len - budget_k). */
+jacap_status jacap_evict_weighted_slots(const jacap_config* cfg, const jacap_batch* batch,
+                                        const jacap_attention* attn, float* acc, int32_t* slots,
+                                        int32_t slot_cap, void* ws, size_t ws_bytes,
+                                        void* stream);
+
 /* Synchronises `stream` and returns the sticky device flags (enum
- * jacap_flags, OR-ed) written by the last jacap_score / jacap_evict that used
- * this workspace. */
+ * jacap_flags, OR-ed) written by the last jacap_score / jacap_evict /
+ * jacap_attend / jacap_attn_weights that used this workspace. */
 jacap_status jacap_read_status(const void* ws, void* stream, uint32_t* flags);
 
 /* Static, human-readable name of a status code. */
@@ -339,7 +475,8 @@ const char* jacap_status_string(jacap_status s);
  * is needed to use the entry points above).
  *
  * While timing is on, every jacap_score / jacap_select / jacap_compact /
- * jacap_evict / jacap_greedy call records a HIP event before and after each phase whose bit
+ * jacap_evict / jacap_greedy / jacap_attend / jacap_attn_weights /
+ * jacap_evict_weighted call records a HIP event before and after each phase whose bit
  * (1u << phase) is set in the mask, on the stream the phase's kernels are
  * launched on; the elapsed time between the two events is that phase's GPU
  * duration. Events are created on the device that is current when the call
@@ -360,7 +497,11 @@ enum jacap_phase {
   JACAP_PHASE_COMPACT = 10,    /* K/V compaction */
   JACAP_PHASE_GREEDY_INIT = 11, /* greedy selection: initial c_i and block maxima */
   JACAP_PHASE_GREEDY = 12,     /* greedy selection: the sequential picks */
-  JACAP_NUM_PHASES = 13
+  JACAP_PHASE_ATTEND = 13,      /* jacap_attend: attention over the chunks of the cache */
+  JACAP_PHASE_ATTEND_JOIN = 14, /* ... join of the chunks, and the accumulation from kept logits */
+  JACAP_PHASE_ATTN_LSE = 15,    /* jacap_attn_weights: the rows' log-sums */
+  JACAP_PHASE_ATTN_SUM = 16,    /* accumulation of the weights (jacap_attend of many rows too) */
+  JACAP_NUM_PHASES = 17
 };
 
 /* Clears the accumulated times and starts recording the phases in

@@ -1,0 +1,177 @@
+// Definitions shared by the attention kernels and their host code: attention
+// of new or drafted tokens over the cache (k_attend.hip) and accumulated
+// attention weights (k_attn_weights.hip).
+//
+// Both use one MFMA arrangement. Logits are formed transposed, S^T = K Q^T, in
+// 16 x 16 tiles (16 tokens of the cache by 16 query rows): lane (m = lane % 16,
+// q = lane / 16) supplies 16-byte pieces of token m's row for A and of query
+// row m for B, and receives the logits of query row m for tokens 4 q .. 4 q + 3.
+// Piece a of a row is its bytes 64 a + 16 q .. + 15: four lanes read 64
+// contiguous bytes per load, and A and B agree on the order of the channels
+// in the contraction, which is all that matters.
+#pragma once
+
+#include "jacap_internal.hpp"
+
+namespace jacap {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kMaxDraft = 512;        // rows per query head jacap_attend takes
+// Rows per KV head (G S) up to which jacap_attend keeps its logits (4 bytes a row and
+// token written, then read) to accumulate from; more rows, and their keys are
+// read again (256 bytes a token at d = 128, bf16) and multiplied again.
+constexpr int kKeepRows = 16;
+constexpr int kAttendChunk = 8192;    // tokens per workgroup of the attention: at most,
+constexpr int kAttendChunkMin = 256;  // ... and at least
+constexpr int kAttendBlocks = 1024;   // chunks shrink until the grid has this many workgroups
+constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
+// The log-sum pass: 16-row tiles per workgroup (their queries in registers),
+// tokens per workgroup.
+constexpr int kLseTilesBf16 = 8, kLseTilesFp32 = 2;
+constexpr int kLseChunk = 8192, kLseChunkMin = 256;
+// The accumulation: 16-token tiles per wave (their keys in registers); the rows are
+// cut into parts of at least kSumRowsMin while the grid is small.
+constexpr int kSumTilesBf16 = 4, kSumTilesFp32 = 2;
+constexpr int kSumRowsMin = 128;
+constexpr int kWeightsBlocks = 1024;  // workgroups both passes aim at
+constexpr int64_t kMaxGrid = (int64_t(1) << 24) - 1;  // workgroups of 256 threads in one launch
+
+// Device view of jacap_attention (and the launch's chunking).
+struct Attn {
+  float c;         // scale * log2(e): logits in powers of two
+  float decay;
+  int accumulate, causal;
+  int R;           // rows per KV head: G * window, row r = head r / window, position r % window
+  const float* row_weight;
+  const uint32_t* tree;  // 32-bit words, little end first
+  int tree_words;        // ... per row
+  int64_t dks, dkl, dkh, dkr, dvs, dvl, dvh, dvr, os, ol, oh, op;
+};
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+
+// How rows of D elements of type T lie in the fragments.
+template <typename T, int D>
+struct Row {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int kBytes = D * sizeof(T);
+  static constexpr int kPieces = kBytes / 64;           // 16-byte pieces per lane of a K or Q row
+  static constexpr int kTiles = kBf16 ? 2 : 1;          // 16-token tiles per step: what one MFMA
+                                                        // of P V contracts (32 bf16; 4 x 4 fp32)
+  static constexpr int kStep = 16 * kTiles;
+  static constexpr int kVBytes = kBytes / 16 < 16 ? kBytes / 16 : 16;  // V bytes per load and lane
+  static constexpr int kVec = kVBytes / (int)sizeof(T);  // channels per load
+  static constexpr int kVLoads = kBytes / 16 / kVBytes;  // loads per V row and lane
+  static constexpr int kVWords = kVBytes / 4;
+  static constexpr int kBlocks = kVLoads * kVec;         // 16-channel blocks of the output
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The 16 x 16 logits tile of 16 tokens and 16 query rows.
+template <typename T, int D>
+__device__ __forceinline__ f32x4 logits(const uint4 (&k)[Row<T, D>::kPieces],
+                                        const uint4 (&q)[Row<T, D>::kPieces]) {
+  f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int a = 0; a < Row<T, D>::kPieces; ++a) {
+    if constexpr (Row<T, D>::kBf16) {
+      z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, k[a]),
+                                                  __builtin_bit_cast(bf8, q[a]), z, 0, 0, 0);
+    } else {
+      const f32x4 kk = __builtin_bit_cast(f32x4, k[a]), qq = __builtin_bit_cast(f32x4, q[a]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) z = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[w], qq[w], z, 0, 0, 0);
+    }
+  }
+  return z;
+}
+
+// Query row r of a unit's R rows (pieces of lane group qg); zeros past the last row.
+template <typename T, int D>
+__device__ __forceinline__ void load_row(const Geo& g, const T* qu, int r, int R, int qg,
+                                         uint4 (&f)[Row<T, D>::kPieces]) {
+  if (r < R) {
+    const int head = r / g.w, p = r - head * g.w;
+    const char* src = reinterpret_cast<const char*>(qu + head * g.qsh + p * g.qsp) + 16 * qg;
+#pragma unroll
+    for (int a = 0; a < Row<T, D>::kPieces; ++a) f[a] = *reinterpret_cast<const uint4*>(src + 64 * a);
+  } else {
+#pragma unroll
+    for (int a = 0; a < Row<T, D>::kPieces; ++a) f[a] = uint4{0, 0, 0, 0};
+  }
+}
+
+// First query row of a unit's G heads.
+template <typename T>
+__device__ __forceinline__ const T* unit_queries(const Geo& g, const Unit& un, const T* q) {
+  return q + un.b * g.qss + un.l * g.qsl + (int64_t)un.h * g.G * g.qsh;
+}
+
+// The status word: bad offsets or lengths of any sequence. Called by every
+// thread of one workgroup.
+__device__ __forceinline__ void write_status(const Geo& g, uint32_t* status) {
+  int bad = 0;
+  for (int b = threadIdx.x; b < g.B; b += kThreads) {
+    const int32_t a = g.seq_off[b], e = g.seq_off[b + 1];
+    const bool ok = offsets_ok(g, a, e);
+    bad |= !ok || !live_ok(g, b, e - a);
+  }
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) *status = bad ? (uint32_t)JACAP_FLAG_BAD_OFFSETS : 0u;
+}
+
+// Running maximum m and sum l of a softmax over one lane's or workgroup's part,
+// in powers of two, joined over parts: exp2(m - ref), with ref finite.
+__device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.0f : m; }
+
+// ---------------------------------------------------------------------------
+// Workspaces (byte offsets; the status word at 0) and launchers
+// ---------------------------------------------------------------------------
+struct AttendSpace {
+  int chunk, splits;   // tokens per workgroup, chunks of the longest sequence
+  int mt;              // 16-row tiles per workgroup
+  int row_blocks;
+  size_t ml;           // float2 [U][R][splits]     (maximum, sum) of a chunk
+  size_t part;         // float  [U][R][splits][D]  its unnormalised output
+  size_t lse;          // float  [U][R]
+  size_t z;            // float  [L][H][R][T]       kept logits (accumulating from few rows)
+  size_t zd;           // float  [U][R][S]          ... and the drafted tokens'
+  size_t total;
+  bool keep;           // logits are kept
+};
+
+struct WeightsSpace {
+  int chunk, chunks, mt, row_blocks;  // the log-sum pass: tokens per workgroup, and rows
+  int tiles;           // the accumulation: 16-token tiles per wave
+  int blocks;          // ... token blocks of the longest sequence
+  int row_splits;      // ... parts the rows are cut into
+  size_t ml;           // float2 [U][R][chunks]
+  size_t lse;          // float [U][R]
+  size_t part;         // float [row_splits][L][H][T]
+  size_t total;
+};
+
+struct AttnLaunch {
+  Launch base;
+  Attn at;
+};
+
+hipError_t launch_attend(const AttnLaunch& A, const AttendSpace& w, const void* q, const void* k,
+                         const void* v, const void* kd, const void* vd, void* out, float* lse,
+                         const float* acc);
+bool attend_joins(const AttnLaunch& A, const AttendSpace& w);
+hipError_t launch_attend_join(const AttnLaunch& A, const AttendSpace& w, void* out, float* lse,
+                              float* acc, float* acc_draft);
+hipError_t launch_attn_lse(const AttnLaunch& A, const WeightsSpace& w, const void* q, const void* k,
+                           const float* acc, float* lse);
+// Adds the rows' weights, given their log-sums, to acc; status may be null.
+hipError_t launch_attn_sum(const AttnLaunch& A, const WeightsSpace& w, const void* q, const void* k,
+                           const float* lse, float* acc, uint32_t* status);
+// The weights the drafted tokens received (after jacap_attend of many rows).
+hipError_t launch_draft_sum(const AttnLaunch& A, const void* q, const void* kd, const float* lse,
+                            float* acc_draft);
+
+}  // namespace jacap

@@ -74,6 +74,8 @@ struct Geo {
   int64_t vsl, vsh, vst;
   int64_t qss, qsl, qsh, qsp;
   int64_t oss, osl, osh, osr;
+  const int32_t* live;          // device [B] current lengths within the offsets' rows, or null
+                                // (selection, compaction and attention: live_unit)
 };
 
 struct Unit {
@@ -101,6 +103,19 @@ __device__ __forceinline__ Unit decode_unit(const Geo& g, int u) {
   const int32_t e = g.seq_off[r.b + 1];
   r.t0 = a;
   r.n = offsets_ok(g, a, e) ? e - a : 0;
+  return r;
+}
+
+// Whether sequence b's current length contradicts its n rows of the cache.
+__device__ __forceinline__ bool live_ok(const Geo& g, int b, int n) {
+  return !g.live || (uint32_t)g.live[b] <= (uint32_t)n;
+}
+
+// decode_unit with n = the sequence's current length (0 where it contradicts
+// the offsets), for the kernels whose caller may give lengths of their own.
+__device__ __forceinline__ Unit live_unit(const Geo& g, int u) {
+  Unit r = decode_unit(g, u);
+  if (g.live) r.n = live_ok(g, r.b, r.n) ? g.live[r.b] : 0;
   return r;
 }
 
@@ -440,6 +455,13 @@ hipError_t launch_select(const Launch& L, const float* scores, int32_t* idx);
 hipError_t launch_select_evicted(const Launch& L, const float* scores, int32_t* slots, int cap);
 hipError_t launch_compact(const Launch& L, const int32_t* idx, const void* k, const void* v,
                           void* ko, void* vo);
+// launch_compact, and the kept tokens' accumulator entries with their rows:
+// entry j of a unit at b * as + l * al + h * ah + j of acc_out, -1 past the kept.
+hipError_t launch_compact_weighted(const Launch& L, const int32_t* idx, const void* k,
+                                   const void* v, void* ko, void* vo, const float* acc,
+                                   float* acc_out, int64_t as, int64_t al, int64_t ah);
+// acc[slot] = -1 for the listed slots of every unit.
+hipError_t launch_mark_slots(const Launch& L, const int32_t* slots, int cap, float* acc);
 hipError_t launch_greedy(const Launch& L, const void* v, int32_t* idx, int32_t* order,
                          double* logdet);
 

@@ -99,7 +99,8 @@ const char* jacap_phase_name(int32_t phase) {
   static const char* names[JACAP_NUM_PHASES] = {"init", "qstats", "kpass", "weights", "gram",
                                                  "gram_reduce", "factor", "refine", "leverage",
                                                  "select", "compact", "greedy_init",
-                                                 "greedy"};
+                                                 "greedy", "attend", "attend_join", "attn_lse",
+                                                 "attn_sum"};
   if (phase < 0 || phase >= JACAP_NUM_PHASES) return "unknown";
   return names[phase];
 }

@@ -1,0 +1,551 @@
+// jacap_attend: attention of the query rows of a decoding step (one new token
+// or a tree of drafted tokens) over the cache and the drafted tokens.
+//
+//   z_ri = scale q_r . k_i,  lse_r = log sum exp(z_r.),  out_r = sum exp(z_r. - lse_r) v
+//
+// One pass over K and V with the running maximum and sum of a softmax. A
+// workgroup takes one unit, 16 MT of its R = G S rows and one chunk of its
+// tokens; its four waves take the chunk's steps in turn, each with a softmax
+// of its own, and no barrier before the chunk's end, where they are joined
+// in LDS. The chunks of long sequences are joined by a second kernel.
+//
+// P V without a transpose in LDS: the second product is also formed
+// transposed, O^T = V^T P^T, and a lane's logits (query row m, tokens 4 q ..
+// 4 q + 3 of each tile) are its operand of P^T as they stand, with the tokens
+// in that order. The operand of V^T then is channel m of a 16-channel block
+// for the same tokens, 4 q .. 4 q + 3. A lane reads kVec consecutive channels
+// kVec m .. of those tokens (whole rows per 16 lanes) and calls channel
+// kVec m + j row m of block j: for bf16 a byte permute per pair of values, and
+// nothing at all for fp32. The result leaves each lane with 4 kVec
+// consecutive channels of its own query row.
+#include <type_traits>
+
+#include <algorithm>
+
+#include "attention.hpp"
+
+namespace jacap {
+
+template <typename T>
+struct AttendArgs {
+  const T *q, *k, *v, *kd, *vd;
+  T* out;
+  float* lse;        // of units of one chunk, or null
+  const float* acc;  // empty slots, or null
+  float2* ml;
+  float* part;
+  float *z, *zd;     // kept logits, or null
+  uint32_t* status;
+};
+
+// The maximum a row's weights refer to is raised only when a logit exceeds it
+// by more than this many powers of two, so most steps neither reduce over lanes nor
+// rescale the output; the weights stay below 2^8, far inside fp32 and bf16.
+constexpr float kLazyMax = 8.0f;
+
+template <typename T, int D, int MT>
+__global__ __launch_bounds__(kThreads) void attend_kernel(Geo g, Attn at, AttendArgs<T> p,
+                                                          int chunk, int splits, int row_blocks) {
+  using W = Row<T, D>;
+  constexpr int NT = W::kTiles, NP = W::kPieces, NL = W::kVLoads, VW = W::kVWords;
+  const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Workgroup -> (unit, chunk, row block): chunk-major; the row blocks of a
+  // (unit, chunk) read the same K and V, and run 8 apart (same XCD, see
+  // grid_unit_chunk_at).
+  int pair = blockIdx.x, rb = 0;
+  if (row_blocks > 1) {
+    const int x = pair % (8 * row_blocks);
+    rb = x >> 3;
+    pair = pair / (8 * row_blocks) * 8 + (x & 7);
+  }
+  if (blockIdx.x == 0) write_status(g, p.status);
+  if (pair >= g.U * splits) return;
+  const int u = pair % g.U, split = pair / g.U;
+  const Unit un = live_unit(g, u);
+  const int S = g.w, R = at.R;
+  const int nsp = max(1, (un.n + chunk - 1) / chunk);
+  if (split >= nsp) return;
+  const int t0 = split * chunk, t1 = min(un.n, t0 + chunk);
+  const bool drafts = split == nsp - 1;  // the last chunk takes the drafted tokens
+
+  // The query rows (lane: row m of each tile).
+  uint4 qf[MT][NP];
+  int row[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    row[i] = (rb * MT + i) * 16 + m;
+    load_row<T, D>(g, unit_queries(g, un, p.q), row[i], R, qg, qf[i]);
+  }
+
+  f32x4 o[MT][W::kBlocks];
+  float mx[MT], thr[MT], ref[MT], l[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    mx[i] = thr[i] = -INFINITY;
+    ref[i] = l[i] = 0.0f;
+#pragma unroll
+    for (int b = 0; b < W::kBlocks; ++b) o[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
+  const T* vb = p.v + un.l * g.vsl + un.h * g.vsh + un.t0 * g.vst;
+  const T* kdb = p.kd + un.b * at.dks + un.l * at.dkl + un.h * at.dkh;
+  const T* vdb = p.vd + un.b * at.dvs + un.l * at.dvl + un.h * at.dvh;
+  const float* accb = p.acc ? p.acc + token_row(g, un) : nullptr;
+
+  uint4 kf[NT][NP];
+  uint32_t vr[NT][4][NL][VW];
+  // Rows [r0, end) of a K / V row range, at most a step of them (zeros past the end).
+  auto load = [&](const T* kbase, const T* vbase, int64_t kst, int64_t vst, int r0, int end) {
+    const int rows = min(W::kStep, end - r0);
+    const int32_t ks = (int32_t)(kst * sizeof(T)), vs = (int32_t)(vst * sizeof(T));
+    const auto kr = buffer_range(kbase + r0 * kst, rows_bytes(rows, ks, W::kBytes));
+    const auto vrs = buffer_range(vbase + r0 * vst, rows_bytes(rows, vs, W::kBytes));
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int a = 0; a < NP; ++a) kf[t][a] = buffer_load16(kr, (16 * t + m) * ks + 64 * a + 16 * qg);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int b = 0; b < NL; ++b)
+          buffer_load_words(vrs, (16 * t + 4 * qg + i) * vs + (16 * b + m) * W::kVBytes, vr[t][i][b]);
+    }
+  };
+
+  // One step. seen: bit 4 t + i, token 16 t + 4 q + i of the step is one that rows may
+  // see; DRAFT: each row sees those of its mask word only (bit = token of the step).
+  auto step = [&](auto draft, uint32_t seen, const uint32_t (&mask)[MT], int r0) {
+    constexpr bool DRAFT = decltype(draft)::value;
+    constexpr uint32_t ALL = (1u << (4 * NT)) - 1;
+    const bool masked = DRAFT || __ballot(seen != ALL) != 0;
+    uint64_t bad[NT][4] = {};  // drafted tokens with a non-finite value, by lane
+    if (masked) {
+      // What no row sees takes no part, whatever it holds: its weight is 0 and so is
+      // its V, since 0 times a NaN or infinity would not be.
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          bool zero = !(seen >> (4 * t + i) & 1);
+          if constexpr (DRAFT) {
+            // ... and a drafted token that some rows see and others do not is added
+            // apart, row by row, if it holds such a value.
+            bool odd = false;
+#pragma unroll
+            for (int b = 0; b < NL; ++b)
+#pragma unroll
+              for (int x = 0; x < VW; ++x) {
+                const uint32_t y = vr[t][i][b][x];
+                odd |= (y & 0x7F800000u) == 0x7F800000u;
+                if (W::kBf16) odd |= (y & 0x7F80u) == 0x7F80u;
+              }
+            bad[t][i] = __ballot(odd && !zero);
+            zero |= (bad[t][i] >> (16 * qg) & 0xFFFF) != 0;
+          }
+#pragma unroll
+          for (int b = 0; b < NL; ++b)
+#pragma unroll
+            for (int x = 0; x < VW; ++x) vr[t][i][b][x] = zero ? 0u : vr[t][i][b][x];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      f32x4 z[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) z[t] = logits<T, D>(kf[t], qf[i]);
+      if (masked) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            bool see = seen >> (4 * t + e) & 1;
+            if constexpr (DRAFT) see = see && (mask[i] >> (16 * t + 4 * qg + e) & 1);
+            z[t][e] = see ? z[t][e] : -INFINITY;
+          }
+      }
+      if (MT == 1 && p.z != nullptr && row[i] < R) {
+        // kept for the accumulation, in powers of two
+        const int end = DRAFT ? S : t1;
+        float* dst = DRAFT ? p.zd + ((int64_t)u * R + row[i]) * S
+                           : p.z + (((int64_t)un.l * g.H + un.h) * R + row[i]) * g.T + un.t0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = r0 + 16 * t + 4 * qg + e;
+            if (j < end) dst[j] = z[t][e] * at.c;
+          }
+      }
+      float top = z[0][0];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, z[t][e]);
+      top *= at.c;
+      if (__ballot(top > thr[i]) != 0) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(mx[i], top), nref = finite_ref(now);
+        const float f = exp2_fast(mx[i] - nref);
+        mx[i] = now;
+        thr[i] = now + kLazyMax;
+        ref[i] = nref;
+        l[i] *= f;
+#pragma unroll
+        for (int b = 0; b < W::kBlocks; ++b) o[i][b] *= f;
+      }
+      f32x4 pw[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pw[t][e] = exp2_fast(__builtin_fmaf(z[t][e], at.c, -ref[i]));
+          l[i] += pw[t][e];
+        }
+      if constexpr (W::kBf16) {
+        bf8 pb;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pb[e] = (__bf16)pw[0][e];
+          pb[4 + e] = (__bf16)pw[NT - 1][e];
+        }
+#pragma unroll
+        for (int j = 0; j < W::kVec; ++j) {
+          const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+          uint4 a;
+          a.x = __builtin_amdgcn_perm(vr[0][1][0][j / 2], vr[0][0][0][j / 2], sel);
+          a.y = __builtin_amdgcn_perm(vr[0][3][0][j / 2], vr[0][2][0][j / 2], sel);
+          a.z = __builtin_amdgcn_perm(vr[NT - 1][1][0][j / 2], vr[NT - 1][0][0][j / 2], sel);
+          a.w = __builtin_amdgcn_perm(vr[NT - 1][3][0][j / 2], vr[NT - 1][2][0][j / 2], sel);
+          o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), pb, o[i][j],
+                                                            0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < NL; ++b)
+#pragma unroll
+          for (int j = 0; j < W::kVec; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              o[i][b * W::kVec + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                  __uint_as_float(vr[0][e][b][j]), pw[0][e], o[i][b * W::kVec + j], 0, 0, 0);
+      }
+      if constexpr (DRAFT) {
+        for (int t = 0; t < NT; ++t)
+          for (int e = 0; e < 4; ++e) {
+            if (bad[t][e] == 0) continue;
+            for (int x = 0; x < 4; ++x) {
+              if ((bad[t][e] >> (16 * x) & 0xFFFF) == 0) continue;
+              const int j = 16 * t + 4 * x + e;
+              // a constant index per trip of the unrolled loops would keep pw in registers;
+              // this path is rare enough for a select
+              float mine = 0.0f;
+#pragma unroll
+              for (int t2 = 0; t2 < NT; ++t2)
+#pragma unroll
+                for (int e2 = 0; e2 < 4; ++e2) mine = t2 == t && e2 == e ? pw[t2][e2] : mine;
+              const float w = __shfl(mine, 16 * x + m);
+              if (mask[i] >> j & 1) {
+                const T* src = vdb + (r0 + j) * at.dvr;
+#pragma unroll
+                for (int b = 0; b < NL; ++b)
+#pragma unroll
+                  for (int jj = 0; jj < W::kVec; ++jj)
+#pragma unroll
+                    for (int e2 = 0; e2 < 4; ++e2) {
+                      const T y = src[(16 * b + 4 * qg + e2) * W::kVec + jj];
+                      float val;
+                      if constexpr (W::kBf16) val = (float)y;
+                      else val = y;
+                      o[i][b * W::kVec + jj][e2] += w * val;
+                    }
+              }
+            }
+          }
+      }
+    }
+  };
+
+  const uint32_t none[MT] = {};
+  const int csteps = (t1 - t0 + W::kStep - 1) / W::kStep;
+  for (int s = wave; s < csteps; s += 4) {
+    const int r0 = t0 + s * W::kStep;
+    load(kb, vb, g.kst, g.vst, r0, t1);
+    uint32_t seen = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = r0 + 16 * t + 4 * qg + e;
+        bool see = j < t1;
+        if (accb) see = see && !(accb[min(j, t1 - 1)] < 0.0f);
+        seen |= (uint32_t)see << (4 * t + e);
+      }
+    step(std::false_type{}, seen, none, r0);
+  }
+  if (drafts) {
+    const int dsteps = (S + W::kStep - 1) / W::kStep;
+    for (int s = (wave + 4 - (csteps & 3)) & 3; s < dsteps; s += 4) {
+      const int r0 = s * W::kStep;
+      load(kdb, vdb, at.dkr, at.dvr, r0, S);
+      uint32_t seen = 0, mask[MT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) seen |= (uint32_t)(r0 + 16 * t + 4 * qg + e < S) << (4 * t + e);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        mask[i] = 0u;
+        if (row[i] < R) {
+          const int pos = row[i] % S;
+          if (at.tree) {
+            const uint32_t* tw = at.tree + ((int64_t)un.b * S + pos) * at.tree_words;
+            mask[i] = tw[r0 >> 5] >> (r0 & 31);
+          } else {
+            const int last = pos - r0;  // sees 0 .. pos
+            mask[i] = last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1u;
+          }
+        }
+      }
+      step(std::true_type{}, seen, mask, r0);
+    }
+  }
+
+  // Join the waves: rows' maxima and sums first, then the output tile by tile.
+  __shared__ float sm[4][16 * MT], sl[4][16 * MT];
+  __shared__ __align__(16) float red[4][16][D + 4];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    l[i] += __shfl_xor(l[i], 16);
+    l[i] += __shfl_xor(l[i], 32);
+    if (qg == 0) {
+      sm[wave][16 * i + m] = mx[i];
+      sl[wave][16 * i + m] = l[i];
+    }
+  }
+  __syncthreads();
+  constexpr int PER = D / 16;  // channels per thread of the joined tile
+  const int jr = tid >> 4, jc = (tid & 15) * PER;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    float top = sm[0][16 * i + m];
+    for (int x = 1; x < 4; ++x) top = fmaxf(top, sm[x][16 * i + m]);
+    const float f = exp2_fast(mx[i] - finite_ref(top));
+    if (i > 0) __syncthreads();
+#pragma unroll
+    for (int b = 0; b < NL; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < W::kVec; j += 4) {
+          const f32x4 x = {o[i][b * W::kVec + j][e] * f, o[i][b * W::kVec + j + 1][e] * f,
+                           o[i][b * W::kVec + j + 2][e] * f, o[i][b * W::kVec + j + 3][e] * f};
+          *reinterpret_cast<f32x4*>(&red[wave][m][(16 * b + 4 * qg + e) * W::kVec + j]) = x;
+        }
+    __syncthreads();
+    const int r = (rb * MT + i) * 16 + jr;
+    float jt = sm[0][16 * i + jr];
+    for (int x = 1; x < 4; ++x) jt = fmaxf(jt, sm[x][16 * i + jr]);
+    const float jref = finite_ref(jt);
+    float sum = 0.0f, val[PER];
+#pragma unroll
+    for (int c = 0; c < PER; ++c) val[c] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      sum += sl[x][16 * i + jr] * exp2_fast(sm[x][16 * i + jr] - jref);
+#pragma unroll
+      for (int c = 0; c < PER; ++c) val[c] += red[x][jr][jc + c];
+    }
+    if (r < R) {
+      const int64_t ur = (int64_t)u * R + r;
+      if ((tid & 15) == 0 && (splits > 1 || p.z)) p.ml[ur * splits + split] = float2{jt, sum};
+      if (nsp == 1) {
+        const int head = r / S, pos = r - head * S;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        T* dst = p.out + un.b * at.os + un.l * at.ol + (int64_t)(un.h * g.G + head) * at.oh +
+                 pos * at.op + jc;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) dst[c] = (T)(val[c] * inv);
+        if (p.lse && (tid & 15) == 0)
+          p.lse[(((int64_t)un.b * g.L + un.l) * g.Hq + un.h * g.G + head) * S + pos] =
+              sum == 0.0f ? -INFINITY : (jt + __log2f(sum)) * kLn2;
+      } else {
+        float* dst = p.part + (ur * splits + split) * D + jc;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) dst[c] = val[c];
+      }
+    }
+  }
+}
+
+template <typename T, int D>
+static hipError_t attend_typed(const AttnLaunch& A, const AttendSpace& w, const void* q,
+                               const void* k, const void* v, const void* kd, const void* vd,
+                               void* out, float* lse, const float* acc) {
+  const Geo& g = A.base.geo;
+  char* ws = A.base.wsp;
+  AttendArgs<T> p{(const T*)q, (const T*)k, (const T*)v, (const T*)kd, (const T*)vd, (T*)out, lse,
+                  acc, ws_ptr<float2>(ws, w.ml), ws_ptr<float>(ws, w.part),
+                  w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
+                  w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, ws_ptr<uint32_t>(ws, 0)};
+  const int64_t pairs = (int64_t)g.U * w.splits;
+  const int64_t grid = w.row_blocks > 1 ? (pairs + 7) / 8 * 8 * w.row_blocks : pairs;
+  attend_kernel<T, D, 1><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, w.chunk,
+                                                                         w.splits, w.row_blocks);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend(const AttnLaunch& A, const AttendSpace& w, const void* q, const void* k,
+                         const void* v, const void* kd, const void* vd, void* out, float* lse,
+                         const float* acc) {
+  const bool wide = A.base.geo.D == 128;
+  if (A.base.cfg->dtype == JACAP_DTYPE_BF16)
+    return wide ? attend_typed<__bf16, 128>(A, w, q, k, v, kd, vd, out, lse, acc)
+                : attend_typed<__bf16, 64>(A, w, q, k, v, kd, vd, out, lse, acc);
+  return wide ? attend_typed<float, 128>(A, w, q, k, v, kd, vd, out, lse, acc)
+              : attend_typed<float, 64>(A, w, q, k, v, kd, vd, out, lse, acc);
+}
+
+// ---------------------------------------------------------------------------
+// Second kernel: joins the chunks of each row (a workgroup per row of a unit),
+// and accumulates the weights of kept logits (a workgroup per kJoinTokens
+// tokens of a unit): p = exp2(z - lse) of every row, with lse joined from the
+// chunks again rather than waited for.
+// ---------------------------------------------------------------------------
+template <typename T>
+struct JoinArgs {
+  T* out;
+  float* lse;             // or null
+  const float2* ml;
+  const float* part;
+  const float *z, *zd;    // or null
+  float* acc;
+  float* acc_draft;       // or null
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, JoinArgs<T> p,
+                                                               int chunk, int splits, int rows_grid,
+                                                               int token_blocks) {
+  const int tid = threadIdx.x, S = g.w, R = at.R;
+  if ((int)blockIdx.x < rows_grid) {
+    const int u = blockIdx.x / R, r = blockIdx.x - u * R;
+    const Unit un = live_unit(g, u);
+    const int nsp = max(1, (un.n + chunk - 1) / chunk);
+    if (nsp == 1) return;  // written by the first kernel
+    const int64_t ur = (int64_t)u * R + r;
+    const float2* ml = p.ml + ur * splits;
+    __shared__ float red[4];
+    float top = -INFINITY;
+    for (int s = tid; s < nsp; s += kThreads) top = fmaxf(top, ml[s].x);
+    top = block_combine(wave_max(top), red, [](float a, float b) { return fmaxf(a, b); });
+    const float ref = finite_ref(top);
+    // thread: 4 channels of every NG-th chunk
+    constexpr int NG = kThreads / (D / 4);
+    const int c = tid % (D / 4) * 4, grp = tid / (D / 4);
+    const float* part = p.part + ur * splits * D + c;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.0f;
+#pragma unroll 4
+    for (int s = grp; s < nsp; s += NG) {
+      const float f = exp2_fast(ml[s].x - ref);
+      l += ml[s].y * f;
+      sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * D) * f;
+    }
+    __shared__ __align__(16) float so[NG][D];
+    __shared__ float sl[NG];
+    *reinterpret_cast<f32x4*>(&so[grp][c]) = sum;
+    if (c == 0) sl[grp] = l;
+    __syncthreads();
+    if (tid < D) {
+      float a = 0.0f, b = 0.0f;
+      for (int x = 0; x < NG; ++x) {
+        a += so[x][tid];
+        b += sl[x];
+      }
+      const int head = r / S, pos = r - head * S;
+      p.out[un.b * at.os + un.l * at.ol + (int64_t)(un.h * g.G + head) * at.oh + pos * at.op + tid] =
+          (T)(b == 0.0f ? 0.0f : a / b);
+      if (p.lse && tid == 0)
+        p.lse[(((int64_t)un.b * g.L + un.l) * g.Hq + un.h * g.G + head) * S + pos] =
+            b == 0.0f ? -INFINITY : (top + __log2f(b)) * kLn2;
+    }
+    return;
+  }
+  const int item = blockIdx.x - rows_grid;
+  const int u = item / token_blocks, blk = item - u * token_blocks;
+  const Unit un = live_unit(g, u);
+  const int t0 = blk * kJoinTokens;
+  if (t0 >= un.n && blk > 0) return;
+  const int nsp = max(1, (un.n + chunk - 1) / chunk);
+  __shared__ float slse[kKeepRows], sw[kKeepRows];
+  {
+    // 16 threads per row
+    const int r = tid >> 4;
+    float top = -INFINITY, l = 0.0f;
+    const float2* ml = p.ml + ((int64_t)u * R + min(r, R - 1)) * splits;
+    for (int s = tid & 15; s < nsp; s += 16) top = fmaxf(top, ml[s].x);
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float ref = finite_ref(top);
+    for (int s = tid & 15; s < nsp; s += 16) l += ml[s].y * exp2_fast(ml[s].x - ref);
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) l += __shfl_xor(l, x);
+    if ((tid & 15) == 0) {
+      float w = 0.0f;
+      if (r < R && l != 0.0f) w = at.row_weight ? at.row_weight[(int64_t)un.b * S + r % S] : 1.0f;
+      sw[r] = w;
+      slse[r] = l == 0.0f ? 0.0f : top + __log2f(l);
+    }
+  }
+  __syncthreads();
+  const int64_t tr = token_row(g, un);
+  const float* z = p.z + (((int64_t)un.l * g.H + un.h) * R) * g.T + un.t0;
+  for (int t = t0 + tid; t < min(un.n, t0 + kJoinTokens); t += kThreads) {
+    const float old = p.acc[tr + t];
+    if (old < 0.0f) continue;
+    float sum = 0.0f;
+    for (int r = 0; r < R; ++r)
+      if (sw[r] != 0.0f) sum = __builtin_fmaf(sw[r], exp2_fast(z[r * g.T + t] - slse[r]), sum);
+    p.acc[tr + t] = at.decay > 0.0f ? __builtin_fmaf(at.decay, old, sum) : sum;
+  }
+  if (blk == 0 && p.acc_draft && tid < S) {
+    float sum = 0.0f;
+    for (int r = 0; r < R; ++r)
+      if (sw[r] != 0.0f)
+        sum = __builtin_fmaf(sw[r], exp2_fast(p.zd[((int64_t)u * R + r) * S + tid] - slse[r]), sum);
+    p.acc_draft[(int64_t)u * S + tid] = sum;
+  }
+}
+
+bool attend_joins(const AttnLaunch& A, const AttendSpace& w) { return w.splits > 1 || w.keep; }
+
+template <typename T, int D>
+static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, void* out, float* lse,
+                             float* acc, float* acc_draft) {
+  const Geo& g = A.base.geo;
+  char* ws = A.base.wsp;
+  JoinArgs<T> p{(T*)out, lse, ws_ptr<float2>(ws, w.ml), ws_ptr<float>(ws, w.part),
+                w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
+                w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, acc, acc_draft};
+  const int rows_grid = w.splits > 1 ? g.U * A.at.R : 0;
+  const int token_blocks = std::max(1, (g.maxn + kJoinTokens - 1) / kJoinTokens);
+  const int64_t grid = rows_grid + (w.keep ? (int64_t)g.U * token_blocks : 0);
+  attend_join_kernel<T, D><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(
+      g, A.at, p, w.chunk, w.splits, rows_grid, token_blocks);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_join(const AttnLaunch& A, const AttendSpace& w, void* out, float* lse,
+                              float* acc, float* acc_draft) {
+  const bool wide = A.base.geo.D == 128;
+  if (A.base.cfg->dtype == JACAP_DTYPE_BF16)
+    return wide ? join_typed<__bf16, 128>(A, w, out, lse, acc, acc_draft)
+                : join_typed<__bf16, 64>(A, w, out, lse, acc, acc_draft);
+  return wide ? join_typed<float, 128>(A, w, out, lse, acc, acc_draft)
+              : join_typed<float, 64>(A, w, out, lse, acc, acc_draft);
+}
+
+}  // namespace jacap

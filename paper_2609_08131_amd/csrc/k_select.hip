@@ -656,7 +656,7 @@ __global__ __launch_bounds__(C::kThreads) void select_kernel(Geo g, const float*
                                                              int32_t* __restrict__ slots, int cap) {
   __shared__ SelShared<C> sh;
   const int u = blockIdx.x, tid = threadIdx.x;
-  const Unit un = decode_unit(g, u);
+  const Unit un = live_unit(g, u);
   int32_t* out = idx + (int64_t)u * budget;
   const int kk_all = min(budget, un.n);
   const float* s = scores + token_row(g, un);
@@ -777,7 +777,7 @@ __global__ __launch_bounds__(kThreads) void evicted_kernel(Geo g, const int32_t*
                                                            int budget, int protect,
                                                            int32_t* __restrict__ slots, int cap) {
   const int u = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
-  const Unit un = decode_unit(g, u);
+  const Unit un = live_unit(g, u);
   const int n = un.n, kk = min(budget, n), ne = n - kk;
   const int npro = min(protect, kk);
   if (ranks_evicted<C>(n - npro, kk - npro)) return;
@@ -823,8 +823,15 @@ hipError_t launch_select_evicted(const Launch& L, const float* scores, int32_t* 
 // Gather: a workgroup copies `rows` consecutive kept rows of one unit; each
 // thread moves one 16-byte piece of UNR rows of K and of V per trip (all
 // loads issued before the stores). STREAM: non-temporal loads and stores, for
-// copies much larger than the caches.
+// copies much larger than the caches. WEIGHTED: the kept tokens' accumulator
+// entries go with their rows (copied by the thread of a row's first piece), and
+// the entries past the kept tokens become empty slots (-1).
 // ---------------------------------------------------------------------------
+struct Weighted {
+  const float* acc;   // [L][H][T]
+  float* out;
+  int64_t as, al, ah;
+};
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <bool STREAM>
@@ -839,13 +846,13 @@ __device__ __forceinline__ void copy_store(char* p, u32x4 x) {
   else *reinterpret_cast<u32x4*>(p) = x;
 }
 
-template <int ROWBYTES, bool STREAM>
+template <int ROWBYTES, bool STREAM, bool WEIGHTED>
 __global__ __launch_bounds__(kThreads) void compact_kernel(Geo g, const int32_t* __restrict__ idx,
                                                            int budget, int rows, int esize,
                                                            const char* __restrict__ k,
                                                            const char* __restrict__ v,
                                                            char* __restrict__ ko,
-                                                           char* __restrict__ vo) {
+                                                           char* __restrict__ vo, Weighted wt) {
   constexpr int PIECES = ROWBYTES / 16;
   constexpr int RPT = kThreads / PIECES;  // rows per trip slice
   constexpr int UNR = 4;
@@ -853,7 +860,7 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Geo g, const int32_t*
   const int j0 = blockIdx.x * rows;
   const int jend = min(budget, j0 + rows);
   if (j0 >= jend) return;
-  const Unit un = decode_unit(g, u);
+  const Unit un = live_unit(g, u);
   const int rr = threadIdx.x / PIECES, off = (threadIdx.x % PIECES) * 16;
   const char* kb = k + ((int64_t)un.l * g.ksl + (int64_t)un.h * g.ksh + un.t0 * g.kst) * esize + off;
   const char* vb = v + ((int64_t)un.l * g.vsl + (int64_t)un.h * g.vsh + un.t0 * g.vst) * esize + off;
@@ -868,6 +875,17 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Geo g, const int32_t*
       const int j = jb + q * RPT + rr;
       t[q] = j < jend ? ix[j] : -1;
       if (t[q] >= un.n) t[q] = -1;  // a position outside the sequence
+    }
+    if constexpr (WEIGHTED) {
+      if (off == 0) {
+        const float* src = wt.acc + token_row(g, un);
+        float* dst = wt.out + un.b * wt.as + un.l * wt.al + un.h * wt.ah;
+#pragma unroll
+        for (int q = 0; q < UNR; ++q) {
+          const int j = jb + q * RPT + rr;
+          if (j < jend) dst[j] = t[q] >= 0 ? src[t[q]] : -1.0f;
+        }
+      }
     }
     u32x4 a[UNR], b[UNR];
 #pragma unroll
@@ -886,8 +904,9 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(Geo g, const int32_t*
   }
 }
 
-hipError_t launch_compact(const Launch& L, const int32_t* idx, const void* k, const void* v,
-                          void* ko, void* vo) {
+template <bool WEIGHTED>
+static hipError_t compact_launch(const Launch& L, const int32_t* idx, const void* k, const void* v,
+                                 void* ko, void* vo, const Weighted& wt) {
   const Geo& g = L.geo;
   const int budget = L.cfg->budget_k;
   if (budget == 0) return hipSuccess;
@@ -899,19 +918,49 @@ hipError_t launch_compact(const Launch& L, const int32_t* idx, const void* k, co
   const dim3 grid((unsigned)((budget + rows - 1) / rows), g.U);
   auto go = [&](auto kern) {
     kern<<<grid, kThreads, 0, L.stream>>>(g, idx, budget, rows, esize, (const char*)k,
-                                          (const char*)v, (char*)ko, (char*)vo);
+                                          (const char*)v, (char*)ko, (char*)vo, wt);
   };
   // Non-temporal above 1 GiB of kept rows (K and V), far beyond L2 and MALL.
   const bool stream = 2 * (int64_t)g.U * budget * rowbytes > (int64_t(1) << 30);
   switch (rowbytes * 2 + (stream ? 1 : 0)) {
-    case 256: go(compact_kernel<128, false>); break;
-    case 257: go(compact_kernel<128, true>); break;
-    case 512: go(compact_kernel<256, false>); break;
-    case 513: go(compact_kernel<256, true>); break;
-    case 1024: go(compact_kernel<512, false>); break;
-    case 1025: go(compact_kernel<512, true>); break;
+    case 256: go(compact_kernel<128, false, WEIGHTED>); break;
+    case 257: go(compact_kernel<128, true, WEIGHTED>); break;
+    case 512: go(compact_kernel<256, false, WEIGHTED>); break;
+    case 513: go(compact_kernel<256, true, WEIGHTED>); break;
+    case 1024: go(compact_kernel<512, false, WEIGHTED>); break;
+    case 1025: go(compact_kernel<512, true, WEIGHTED>); break;
     default: return hipErrorInvalidValue;
   }
+  return hipGetLastError();
+}
+
+hipError_t launch_compact(const Launch& L, const int32_t* idx, const void* k, const void* v,
+                          void* ko, void* vo) {
+  return compact_launch<false>(L, idx, k, v, ko, vo, Weighted{});
+}
+
+hipError_t launch_compact_weighted(const Launch& L, const int32_t* idx, const void* k,
+                                   const void* v, void* ko, void* vo, const float* acc,
+                                   float* acc_out, int64_t as, int64_t al, int64_t ah) {
+  return compact_launch<true>(L, idx, k, v, ko, vo, Weighted{acc, acc_out, as, al, ah});
+}
+
+// Empty slots of a cache refilled in place: the listed positions (-1: none) of
+// each unit, whose lists the selection has written before.
+__global__ __launch_bounds__(kThreads) void mark_slots_kernel(Geo g,
+                                                              const int32_t* __restrict__ slots,
+                                                              int cap, float* __restrict__ acc) {
+  const int u = blockIdx.y, j = blockIdx.x * kThreads + threadIdx.x;
+  if (j >= cap) return;
+  const Unit un = live_unit(g, u);
+  const int t = slots[(int64_t)u * cap + j];
+  if (t >= 0 && t < un.n) acc[token_row(g, un) + t] = -1.0f;
+}
+
+hipError_t launch_mark_slots(const Launch& L, const int32_t* slots, int cap, float* acc) {
+  if (cap == 0) return hipSuccess;
+  mark_slots_kernel<<<dim3((cap + kThreads - 1) / kThreads, L.geo.U), kThreads, 0, L.stream>>>(
+      L.geo, slots, cap, acc);
   return hipGetLastError();
 }
 

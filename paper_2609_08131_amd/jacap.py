@@ -75,6 +75,23 @@ class Batch(ctypes.Structure):
     ]
 
 
+class Attention(ctypes.Structure):
+    _fields_ = [
+        ("scale", ctypes.c_float), ("decay", ctypes.c_float),
+        ("accumulate", ctypes.c_int32), ("causal", ctypes.c_int32),
+        ("live_lens", ctypes.c_void_p), ("row_weight", ctypes.c_void_p),
+        ("tree", ctypes.c_void_p),
+        ("dk_stride_seq", ctypes.c_int64), ("dk_stride_layer", ctypes.c_int64),
+        ("dk_stride_head", ctypes.c_int64), ("dk_stride_row", ctypes.c_int64),
+        ("dv_stride_seq", ctypes.c_int64), ("dv_stride_layer", ctypes.c_int64),
+        ("dv_stride_head", ctypes.c_int64), ("dv_stride_row", ctypes.c_int64),
+        ("o_stride_seq", ctypes.c_int64), ("o_stride_layer", ctypes.c_int64),
+        ("o_stride_head", ctypes.c_int64), ("o_stride_pos", ctypes.c_int64),
+        ("a_stride_seq", ctypes.c_int64), ("a_stride_layer", ctypes.c_int64),
+        ("a_stride_head", ctypes.c_int64),
+    ]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -82,6 +99,7 @@ def _load() -> ctypes.CDLL:
             "`python -m paper_2609_08131_amd.build` (there is no CPU fallback)")
     lib = ctypes.CDLL(LIB_PATH)
     P, C, B = ctypes.c_void_p, ctypes.POINTER(Config), ctypes.POINTER(Batch)
+    A = ctypes.POINTER(Attention)
     sz = ctypes.c_size_t
     sigs = {
         "jacap_workspace_size": [C, B, ctypes.POINTER(sz)],
@@ -97,6 +115,13 @@ def _load() -> ctypes.CDLL:
         "jacap_greedy": [C, B, P, P, P, P, P, P, P, sz, P],
         "jacap_stream_read": [P, sz, P, P],
         "jacap_evict_noalloc": [C, B, P, P, P, P, P, P, P, P, P],
+        "jacap_attend_workspace_size": [C, B, A, ctypes.POINTER(sz)],
+        "jacap_attend": [C, B, A, P, P, P, P, P, P, P, P, P, P, sz, P],
+        "jacap_attn_weights_workspace_size": [C, B, A, ctypes.POINTER(sz)],
+        "jacap_attn_weights": [C, B, A, P, P, P, P, P, P, sz, P],
+        "jacap_evict_weighted_workspace_size": [C, B, A, ctypes.POINTER(sz)],
+        "jacap_evict_weighted": [C, B, A, P, P, P, P, P, P, P, P],
+        "jacap_evict_weighted_slots": [C, B, A, P, P, ctypes.c_int32, P, sz, P],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -118,8 +143,11 @@ EXPORTED = ("jacap_workspace_size", "jacap_score", "jacap_score_from_stats", "ja
             "jacap_compact", "jacap_evict", "jacap_read_status", "jacap_status_string",
             "jacap_timing_start", "jacap_timing_stop", "jacap_phase_name",
             "jacap_greedy_workspace_size", "jacap_greedy", "jacap_stream_read",
-            "jacap_select_evicted", "jacap_evict_slots", "jacap_evict_noalloc")
-NUM_PHASES = 13   # enum jacap_phase
+            "jacap_select_evicted", "jacap_evict_slots", "jacap_evict_noalloc",
+            "jacap_attend_workspace_size", "jacap_attend", "jacap_attn_weights_workspace_size",
+            "jacap_attn_weights", "jacap_evict_weighted_workspace_size", "jacap_evict_weighted",
+            "jacap_evict_weighted_slots")
+NUM_PHASES = 17   # enum jacap_phase
 
 
 def status_string(code: int) -> str:
@@ -314,6 +342,54 @@ def read_status(ws: torch.Tensor, stream=None) -> int:
     return int(f.value)
 
 
+def attend_workspace_size(cfg: Config, batch: Batch, attn: Attention) -> int:
+    n = ctypes.c_size_t(0)
+    _check("jacap_attend_workspace_size", _lib.jacap_attend_workspace_size(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(n)))
+    return int(n.value)
+
+
+def attend(cfg, batch, attn, q, k, v, kd, vd, out, lse, acc, acc_draft, ws, stream=None) -> None:
+    _check("jacap_attend", _lib.jacap_attend(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), _ptr(q), _ptr(k), _ptr(v),
+        _ptr(kd), _ptr(vd), _ptr(out), _ptr(lse), _ptr(acc), _ptr(acc_draft), _ptr(ws),
+        ws.numel() if ws is not None else 0, _stream(stream)))
+
+
+def attn_weights_workspace_size(cfg: Config, batch: Batch, attn: Attention) -> int:
+    n = ctypes.c_size_t(0)
+    _check("jacap_attn_weights_workspace_size", _lib.jacap_attn_weights_workspace_size(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(n)))
+    return int(n.value)
+
+
+def attn_weights(cfg, batch, attn, q, k, lse_in, lse_out, acc, ws, stream=None) -> None:
+    _check("jacap_attn_weights", _lib.jacap_attn_weights(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), _ptr(q), _ptr(k),
+        _ptr(lse_in), _ptr(lse_out), _ptr(acc), _ptr(ws), ws.numel() if ws is not None else 0,
+        _stream(stream)))
+
+
+def evict_weighted_workspace_size(cfg: Config, batch: Batch, attn: Attention) -> int:
+    n = ctypes.c_size_t(0)
+    _check("jacap_evict_weighted_workspace_size", _lib.jacap_evict_weighted_workspace_size(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(n)))
+    return int(n.value)
+
+
+def evict_weighted(cfg, batch, attn, acc, k, v, idx, k_out, v_out, acc_out, stream=None) -> None:
+    _check("jacap_evict_weighted", _lib.jacap_evict_weighted(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), _ptr(acc), _ptr(k), _ptr(v),
+        _ptr(idx), _ptr(k_out), _ptr(v_out), _ptr(acc_out), _stream(stream)))
+
+
+def evict_weighted_slots(cfg, batch, attn, acc, slots, ws, stream=None) -> None:
+    """slots: int32 [B][L][H][slot_cap] (the last dimension is the capacity)."""
+    _check("jacap_evict_weighted_slots", _lib.jacap_evict_weighted_slots(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), _ptr(acc), _ptr(slots),
+        int(slots.shape[-1]), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)))
+
+
 # ---------------------------------------------------------------------------
 # Convenience: allocate outputs and run the whole path on torch tensors
 # ---------------------------------------------------------------------------
@@ -357,7 +433,7 @@ def alloc_slots(prob: Problem, seq_lens) -> torch.Tensor:
     """int32 [B][L][H][max(0, max_seq_len - budget)] for select_evicted / evict_slots."""
     B, L, H = prob.idx.shape[:3]
     cap = max(0, int(prob.batch.max_seq_len) - int(prob.cfg.budget_k))
-    return torch.empty((B, L, H, max(cap, 1)), dtype=torch.int32, device=prob.scores.device)
+    return torch.empty((B, L, H, max(cap, 1)), dtype=torch.int32, device=prob.idx.device)
 
 
 def run_evict_slots(prob: Problem, slots, q_win, k, v, stream=None) -> None:
@@ -394,6 +470,255 @@ def prepare_greedy(q_win, k, v, seq_offsets, seq_lens, params: Params) -> Greedy
 
 def run_greedy(prob: GreedyProblem, q_win, k, v, stream=None) -> None:
     greedy(prob.cfg, prob.batch, q_win, k, v, prob.idx, prob.order, prob.logdet, prob.ws, stream)
+
+
+# ---------------------------------------------------------------------------
+# Attention over the cache, and eviction by accumulated attention weight
+# ---------------------------------------------------------------------------
+
+@dataclasses.dataclass
+class AttentionParams:
+    """Parameters of attend / attn_weights (see jacap_attention in include/jacap.h)."""
+
+    scale: Optional[float] = None       # None: 1 / sqrt(head_dim)
+    decay: float = 1.0                  # what accumulators are multiplied by (0: overwritten)
+    accumulate: bool = False            # attend: add the rows' weights to the accumulators
+    causal: bool = True                 # attn_weights: rows are the sequence's last positions
+    live_lens: Optional[torch.Tensor] = None    # device int32 [B]: current sequence lengths
+    row_weight: Optional[torch.Tensor] = None   # device float32 [B][rows]
+    tree: Optional[torch.Tensor] = None         # device int64 [B][rows][ceil(rows / 64)] masks
+
+
+def _expect(name: str, t: torch.Tensor, shape, dtype, device, dense: bool = True) -> None:
+    """A tensor of this shape, dtype and device (dense: contiguous)."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}; got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not dense and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: head_dim must be contiguous")
+
+
+def _cache_checks(seq_offsets, seq_lens, k, *more) -> None:
+    """The cache and what goes with it: shapes, dtype, and all on the current device."""
+    if k.dim() != 4:
+        raise ValueError("k must be [L][H_kv][T_total][d]")
+    if not k.is_cuda or k.device.index != torch.cuda.current_device():
+        raise ValueError(f"k is on {k.device}, not on the current device")
+    if k.dtype not in _DTYPE_CODE:
+        raise ValueError("q, k, v must share a dtype: float32 or bfloat16")
+    if sum(int(n) for n in seq_lens) != k.shape[2]:
+        raise ValueError(f"seq_lens must sum to k's {k.shape[2]} rows")
+    _expect("seq_offsets", seq_offsets, (len(seq_lens) + 1,), torch.int32, k.device)
+    for name, t, shape in more:
+        _expect(name, t, shape, k.dtype, k.device, dense=False)
+
+
+def _attention(p: AttentionParams, B: int, rows: int, d: int, device) -> Attention:
+    a = Attention()
+    a.scale = float(p.scale) if p.scale is not None else d ** -0.5
+    a.decay = float(p.decay)
+    a.accumulate, a.causal = int(bool(p.accumulate)), int(bool(p.causal))
+    if p.live_lens is not None:
+        _expect("live_lens", p.live_lens, (B,), torch.int32, device)
+        a.live_lens = p.live_lens.data_ptr()
+    if p.row_weight is not None:
+        _expect("row_weight", p.row_weight, (B, rows), torch.float32, device)
+        a.row_weight = p.row_weight.data_ptr()
+    if p.tree is not None:
+        _expect("tree", p.tree, (B, rows, (rows + 63) // 64), torch.int64, device)
+        a.tree = p.tree.data_ptr()
+    return a
+
+
+def _workspace(nbytes: int, device) -> torch.Tensor:
+    ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    assert ws.data_ptr() % 256 == 0
+    return ws
+
+
+def _strides(a, prefix: str, t: torch.Tensor) -> None:
+    for name, x in zip(("seq", "layer", "head", "row"), t.stride()):
+        setattr(a, f"{prefix}_stride_{name}", x)
+
+
+@dataclasses.dataclass
+class AttendProblem:
+    """Descriptors, outputs and workspace of jacap_attend for one batch. The
+    parameters' tensors are kept with it: the descriptors hold their addresses."""
+
+    cfg: Config
+    batch: Batch
+    attn: Attention
+    out: torch.Tensor                     # [B][L][H_q][S][d]
+    lse: torch.Tensor                     # float32 [B][L][H_q][S]
+    acc_draft: Optional[torch.Tensor]     # float32 [B][L][H_kv][S], with accumulate
+    ws: torch.Tensor
+    params: AttentionParams
+    seq_offsets: torch.Tensor
+
+
+def prepare_attend(q, k, v, kd, vd, seq_offsets, seq_lens, params: AttentionParams) -> AttendProblem:
+    """seq_lens: the rows of the cache each sequence owns (their current lengths
+    where params.live_lens gives none). q [B][L][H_q][S][d]; kd, vd [B][L][H_kv][S][d]."""
+    B, L, Hq, S, d = q.shape
+    H = k.shape[1]
+    _cache_checks(seq_offsets, seq_lens, k, ("v", v, k.shape),
+                  ("q", q, (len(seq_lens), k.shape[0], Hq, S, k.shape[3])),
+                  ("kd", kd, (B, L, H, S, d)), ("vd", vd, (B, L, H, S, d)))
+    cfg = make_config(q, k, Params(budget_k=0))
+    batch = make_batch(seq_offsets, seq_lens, q, k, v)
+    attn = _attention(params, B, S, d, k.device)
+    out = torch.empty((B, L, Hq, S, d), dtype=k.dtype, device=k.device)
+    _strides(attn, "dk", kd)
+    _strides(attn, "dv", vd)
+    attn.o_stride_seq, attn.o_stride_layer, attn.o_stride_head, attn.o_stride_pos = out.stride()[:4]
+    ws = _workspace(attend_workspace_size(cfg, batch, attn), k.device)
+    lse = torch.empty((B, L, Hq, S), dtype=torch.float32, device=k.device)
+    acc_draft = torch.empty((B, L, H, S), dtype=torch.float32, device=k.device) \
+        if params.accumulate else None
+    return AttendProblem(cfg, batch, attn, out, lse, acc_draft, ws, params, seq_offsets)
+
+
+def _expect_strides(prob, **tensors) -> None:
+    """Tensors of a run: laid out as those the problem was prepared with."""
+    for name, (t, shape, strides) in tensors.items():
+        _expect(name, t, shape, _TORCH_DTYPE[prob.cfg.dtype], prob.ws.device, dense=False)
+        if any(n > 1 and x != y for n, x, y in zip(shape, t.stride(), strides)):
+            raise ValueError(f"{name} must have the strides the problem was prepared with")
+
+
+def _kv_layout(prob, which: str):
+    c, b = prob.cfg, prob.batch
+    return ((c.num_layers, c.num_kv_heads, b.total_tokens, c.head_dim),
+            tuple(getattr(b, f"{which}_stride_{x}") for x in ("layer", "head", "token")))
+
+
+def _q_layout(prob):
+    c, b = prob.cfg, prob.batch
+    return ((b.num_seqs, c.num_layers, c.num_q_heads, c.window, c.head_dim),
+            (b.q_stride_seq, b.q_stride_layer, b.q_stride_head, b.q_stride_pos))
+
+
+def _draft_layout(prob, which: str):
+    c, b, a = prob.cfg, prob.batch, prob.attn
+    return ((b.num_seqs, c.num_layers, c.num_kv_heads, c.window, c.head_dim),
+            tuple(getattr(a, f"{which}_stride_{x}") for x in ("seq", "layer", "head", "row")))
+
+
+def _expect_acc(prob, acc) -> None:
+    c, b = prob.cfg, prob.batch
+    _expect("acc", acc, (c.num_layers, c.num_kv_heads, b.total_tokens), torch.float32,
+            prob.ws.device)
+
+
+def run_attend(prob: AttendProblem, q, k, v, kd, vd, acc=None, stream=None) -> None:
+    _expect_strides(prob, q=(q, *_q_layout(prob)), k=(k, *_kv_layout(prob, "k")),
+                    v=(v, *_kv_layout(prob, "v")), kd=(kd, *_draft_layout(prob, "dk")),
+                    vd=(vd, *_draft_layout(prob, "dv")))
+    if acc is not None or prob.attn.accumulate:
+        _expect_acc(prob, acc)
+    attend(prob.cfg, prob.batch, prob.attn, q, k, v, kd, vd, prob.out, prob.lse, acc,
+           prob.acc_draft, prob.ws, stream)
+
+
+@dataclasses.dataclass
+class AttnWeightsProblem:
+    """Descriptors, outputs and workspace of jacap_attn_weights for one batch."""
+
+    cfg: Config
+    batch: Batch
+    attn: Attention
+    lse: torch.Tensor       # float32 [B][L][H_q][w], written where a run gives none
+    ws: torch.Tensor
+    params: AttentionParams
+    seq_offsets: torch.Tensor
+
+
+def prepare_attn_weights(q, k, seq_offsets, seq_lens, params: AttentionParams) -> AttnWeightsProblem:
+    """seq_lens as prepare_attend; q [B][L][H_q][w][d]."""
+    B, L, Hq, w, d = q.shape
+    _cache_checks(seq_offsets, seq_lens, k, ("q", q, (len(seq_lens), k.shape[0], Hq, w, k.shape[3])))
+    cfg = make_config(q, k, Params(budget_k=0))
+    batch = make_batch(seq_offsets, seq_lens, q, k, k)
+    attn = _attention(params, B, w, d, k.device)
+    ws = _workspace(attn_weights_workspace_size(cfg, batch, attn), k.device)
+    lse = torch.empty((B, L, Hq, w), dtype=torch.float32, device=k.device)
+    return AttnWeightsProblem(cfg, batch, attn, lse, ws, params, seq_offsets)
+
+
+def run_attn_weights(prob: AttnWeightsProblem, q, k, acc, lse=None, stream=None) -> None:
+    """lse: the rows' log-sums if they are known (else computed into prob.lse)."""
+    _expect_strides(prob, q=(q, *_q_layout(prob)), k=(k, *_kv_layout(prob, "k")))
+    _expect_acc(prob, acc)
+    if lse is not None:
+        _expect("lse", lse, prob.lse.shape, torch.float32, prob.ws.device)
+    attn_weights(prob.cfg, prob.batch, prob.attn, q, k, lse, prob.lse if lse is None else None,
+                 acc, prob.ws, stream)
+
+
+@dataclasses.dataclass
+class EvictWeightedProblem:
+    """Descriptors, outputs and workspace of the eviction by accumulated weight."""
+
+    cfg: Config
+    batch: Batch
+    attn: Attention
+    idx: torch.Tensor       # int32 [B][L][H_kv][budget]
+    k_out: torch.Tensor     # [B][L][H_kv][budget][d]
+    v_out: torch.Tensor
+    acc_out: torch.Tensor   # float32 [B][L][H_kv][budget]
+    ws: torch.Tensor
+    live_lens: Optional[torch.Tensor]
+    seq_offsets: torch.Tensor
+
+
+def prepare_evict_weighted(k, v, seq_offsets, seq_lens, budget: int, protect_last: int = 0,
+                           live_lens=None, k_out=None, v_out=None, acc_out=None) -> EvictWeightedProblem:
+    """seq_lens as prepare_attend. k_out, v_out [B][L][H_kv][budget][d] and acc_out
+    [B][L][H_kv][budget]: views to write the retained cache to (k_out and v_out of the
+    same strides), allocated dense where not given."""
+    L, H, T, d = k.shape
+    B, dev, kb = len(seq_lens), k.device, max(int(budget), 0)
+    _cache_checks(seq_offsets, seq_lens, k, ("v", v, k.shape))
+    rows = (B, L, H, kb)
+    idx = torch.empty((B, L, H, max(kb, 1)), dtype=torch.int32, device=dev)[..., :kb]
+    if k_out is None:
+        k_out = torch.empty((B, L, H, max(kb, 1), d), dtype=k.dtype, device=dev)[..., :kb, :]
+    if v_out is None:
+        v_out = torch.empty_strided(k_out.shape, k_out.stride(), dtype=k.dtype, device=dev)
+    if acc_out is None:
+        acc_out = torch.empty((B, L, H, max(kb, 1)), dtype=torch.float32, device=dev)[..., :kb]
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        _expect(name, t, (*rows, d), k.dtype, dev, dense=False)
+    if k_out.stride() != v_out.stride():
+        raise ValueError("k_out and v_out must have the same strides")
+    _expect("acc_out", acc_out, rows, torch.float32, dev, dense=False)
+    dummy = k.new_empty((B, L, H, 1, d))   # the eviction reads no queries: their shape only
+    cfg = make_config(dummy, k, Params(budget_k=int(budget), protect_last=protect_last))
+    batch = make_batch(seq_offsets, seq_lens, dummy, k, v, out=k_out)
+    attn = _attention(AttentionParams(live_lens=live_lens), B, 1, d, dev)
+    attn.a_stride_seq, attn.a_stride_layer, attn.a_stride_head = acc_out.stride()[:3]
+    ws = _workspace(evict_weighted_workspace_size(cfg, batch, attn), dev)
+    return EvictWeightedProblem(cfg, batch, attn, idx, k_out, v_out, acc_out, ws, live_lens,
+                                seq_offsets)
+
+
+def run_evict_weighted(prob: EvictWeightedProblem, acc, k, v, stream=None) -> None:
+    _expect_strides(prob, k=(k, *_kv_layout(prob, "k")), v=(v, *_kv_layout(prob, "v")))
+    _expect_acc(prob, acc)
+    evict_weighted(prob.cfg, prob.batch, prob.attn, acc, k, v, prob.idx, prob.k_out, prob.v_out,
+                   prob.acc_out, stream)
+
+
+def run_evict_weighted_slots(prob: EvictWeightedProblem, acc, slots, stream=None) -> None:
+    """slots: int32 [B][L][H_kv][cap], cap >= max_seq_len - budget (alloc_slots); acc is updated."""
+    _expect_acc(prob, acc)
+    _expect("slots", slots, (*prob.idx.shape[:3], slots.shape[-1]), torch.int32, prob.ws.device)
+    evict_weighted_slots(prob.cfg, prob.batch, prob.attn, acc, slots, prob.ws, stream)
 
 
 # ---------------------------------------------------------------------------
