@@ -125,7 +125,7 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   const Geo& g = A.base.geo;
   const int64_t UR = (int64_t)g.U * A.at.R, LHT = (int64_t)g.L * g.H * g.T;
   size_t o = 256;
-  w->mt = 1;
+  w->mt = A.at.R <= 16 ? 1 : 2;
   w->row_blocks = (A.at.R + 16 * w->mt - 1) / (16 * w->mt);
   w->chunk = chunk_tokens(g, w->row_blocks, kAttendChunk, kAttendChunkMin, kAttendBlocks);
   w->splits = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);

@@ -43,8 +43,11 @@ struct AttendArgs {
 // rescale the output; the weights stay below 2^8, far inside fp32 and bf16.
 constexpr float kLazyMax = 8.0f;
 
+// Four floats at a 4-byte aligned address.
+struct __attribute__((packed, aligned(4))) Float4 { float x, y, z, w; };
+
 template <typename T, int D, int MT>
-__global__ __launch_bounds__(kThreads) void attend_kernel(Geo g, Attn at, AttendArgs<T> p,
+__global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, AttendArgs<T> p,
                                                           int chunk, int splits, int row_blocks) {
   using W = Row<T, D>;
   constexpr int NT = W::kTiles, NP = W::kPieces, NL = W::kVLoads, VW = W::kVWords;
@@ -96,39 +99,59 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geo g, Attn at, Attend
 
   uint4 kf[NT][NP];
   uint32_t vr[NT][4][NL][VW];
-  // Rows [r0, end) of a K / V row range, at most a step of them (zeros past the end).
-  auto load = [&](const T* kbase, const T* vbase, int64_t kst, int64_t vst, int r0, int end) {
-    const int rows = min(W::kStep, end - r0);
-    const int32_t ks = (int32_t)(kst * sizeof(T)), vs = (int32_t)(vst * sizeof(T));
-    const auto kr = buffer_range(kbase + r0 * kst, rows_bytes(rows, ks, W::kBytes));
-    const auto vrs = buffer_range(vbase + r0 * vst, rows_bytes(rows, vs, W::kBytes));
+  // Rows [r0, end) of a K or V row range, at most a step of them (zeros past the end).
+  auto load_k = [&](const T* base, int64_t stride, int r0, int end) {
+    const int32_t bytes = (int32_t)(stride * sizeof(T));
+    const auto rs = buffer_range(base + r0 * stride,
+                                 rows_bytes(min(W::kStep, end - r0), bytes, W::kBytes));
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int a = 0; a < NP; ++a) kf[t][a] = buffer_load16(kr, (16 * t + m) * ks + 64 * a + 16 * qg);
+      for (int a = 0; a < NP; ++a) kf[t][a] = buffer_load16(rs, (16 * t + m) * bytes + 64 * a + 16 * qg);
+  };
+  auto load_v = [&](const T* base, int64_t stride, int r0, int end) {
+    const int32_t bytes = (int32_t)(stride * sizeof(T));
+    const auto rs = buffer_range(base + r0 * stride,
+                                 rows_bytes(min(W::kStep, end - r0), bytes, W::kBytes));
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int b = 0; b < NL; ++b)
-          buffer_load_words(vrs, (16 * t + 4 * qg + i) * vs + (16 * b + m) * W::kVBytes, vr[t][i][b]);
-    }
+          buffer_load_words(rs, (16 * t + 4 * qg + i) * bytes + (16 * b + m) * W::kVBytes, vr[t][i][b]);
+  };
+  // The accumulator entry of token r0 + lane % kStep (0 past the end): one load per
+  // step; a ballot of their signs is the step's hidden tokens.
+  auto load_acc = [&](int r0, int end) {
+    return buffer_load_f32(buffer_range(accb + r0, 4 * max(0, min(W::kStep, end - r0))),
+                           4 * (lane & (W::kStep - 1)));
   };
 
-  // One step. seen: bit 4 t + i, token 16 t + 4 q + i of the step is one that rows may
-  // see; DRAFT: each row sees those of its mask word only (bit = token of the step).
-  auto step = [&](auto draft, uint32_t seen, const uint32_t (&mask)[MT], int r0) {
+  // One step over the K and V rows held. vis: bit j, token j of the step is one that rows
+  // may see; DRAFT: each row sees those of its mask only. `fetch_k` and
+  // `fetch_v` are called where the registers of K and V have been read.
+  auto step = [&](auto draft, uint32_t vis, const uint32_t (&mask)[MT], int r0, auto fetch_k,
+                  auto fetch_v) {
     constexpr bool DRAFT = decltype(draft)::value;
-    constexpr uint32_t ALL = (1u << (4 * NT)) - 1;
-    const bool masked = DRAFT || __ballot(seen != ALL) != 0;
-    uint64_t bad[NT][4] = {};  // drafted tokens with a non-finite value, by lane
+    constexpr uint32_t ALL = W::kStep == 32 ? ~0u : (1u << (W::kStep & 31)) - 1;
+    const bool masked = DRAFT || vis != ALL;
+    f32x4 z[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) z[i][t] = logits<T, D>(kf[t], qf[i]);
+    fetch_k();
+    const uint32_t mine = vis >> (4 * qg);  // bit 16 t + e: token 16 t + 4 q + e
+    uint64_t bad[NT][4] = {};               // drafted tokens with a non-finite value, by lane
     if (masked) {
       // What no row sees takes no part, whatever it holds: its weight is 0 and so is
       // its V, since 0 times a NaN or infinity would not be.
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          bool zero = !(seen >> (4 * t + i) & 1);
+        for (int e = 0; e < 4; ++e) {
+          bool zero = !(mine >> (16 * t + e) & 1);
           if constexpr (DRAFT) {
             // ... and a drafted token that some rows see and others do not is added
             // apart, row by row, if it holds such a value.
@@ -137,52 +160,50 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geo g, Attn at, Attend
             for (int b = 0; b < NL; ++b)
 #pragma unroll
               for (int x = 0; x < VW; ++x) {
-                const uint32_t y = vr[t][i][b][x];
+                const uint32_t y = vr[t][e][b][x];
                 odd |= (y & 0x7F800000u) == 0x7F800000u;
                 if (W::kBf16) odd |= (y & 0x7F80u) == 0x7F80u;
               }
-            bad[t][i] = __ballot(odd && !zero);
-            zero |= (bad[t][i] >> (16 * qg) & 0xFFFF) != 0;
+            bad[t][e] = __ballot(odd && !zero);
+            zero |= (bad[t][e] >> (16 * qg) & 0xFFFF) != 0;
           }
 #pragma unroll
           for (int b = 0; b < NL; ++b)
 #pragma unroll
-            for (int x = 0; x < VW; ++x) vr[t][i][b][x] = zero ? 0u : vr[t][i][b][x];
+            for (int x = 0; x < VW; ++x) vr[t][e][b][x] = zero ? 0u : vr[t][e][b][x];
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            bool see = mine >> (16 * t + e) & 1;
+            if constexpr (DRAFT) see = see && (mask[i] >> (16 * t + 4 * qg + e) & 1);
+            z[i][t][e] = see ? z[i][t][e] : -INFINITY;
+          }
         }
+    }
+    if (MT == 1 && p.z != nullptr && row[0] < R) {
+      // kept for the accumulation, in powers of two
+      const int end = (DRAFT ? S : t1) - r0;
+      float* dst = (DRAFT ? p.zd + ((int64_t)u * R + row[0]) * S
+                          : p.z + (((int64_t)un.l * g.H + un.h) * R + row[0]) * g.T + un.t0) + r0;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int j = 16 * t + 4 * qg;
+        if (j + 4 <= end) {
+          *reinterpret_cast<Float4*>(dst + j) =
+              Float4{z[0][t][0] * at.c, z[0][t][1] * at.c, z[0][t][2] * at.c, z[0][t][3] * at.c};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (j + e < end) dst[j + e] = z[0][t][e] * at.c;
+        }
+      }
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      f32x4 z[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) z[t] = logits<T, D>(kf[t], qf[i]);
-      if (masked) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            bool see = seen >> (4 * t + e) & 1;
-            if constexpr (DRAFT) see = see && (mask[i] >> (16 * t + 4 * qg + e) & 1);
-            z[t][e] = see ? z[t][e] : -INFINITY;
-          }
-      }
-      if (MT == 1 && p.z != nullptr && row[i] < R) {
-        // kept for the accumulation, in powers of two
-        const int end = DRAFT ? S : t1;
-        float* dst = DRAFT ? p.zd + ((int64_t)u * R + row[i]) * S
-                           : p.z + (((int64_t)un.l * g.H + un.h) * R + row[i]) * g.T + un.t0;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = r0 + 16 * t + 4 * qg + e;
-            if (j < end) dst[j] = z[t][e] * at.c;
-          }
-      }
-      float top = z[0][0];
+      float top = z[i][0][0];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, z[t][e]);
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, z[i][t][e]);
       top *= at.c;
       if (__ballot(top > thr[i]) != 0) {
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -196,105 +217,109 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geo g, Attn at, Attend
 #pragma unroll
         for (int b = 0; b < W::kBlocks; ++b) o[i][b] *= f;
       }
-      f32x4 pw[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          pw[t][e] = exp2_fast(__builtin_fmaf(z[t][e], at.c, -ref[i]));
-          l[i] += pw[t][e];
+          z[i][t][e] = exp2_fast(__builtin_fmaf(z[i][t][e], at.c, -ref[i]));
+          l[i] += z[i][t][e];
         }
-      if constexpr (W::kBf16) {
-        bf8 pb;
+    }
+    if constexpr (W::kBf16) {
+      bf8 pb[MT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          pb[e] = (__bf16)pw[0][e];
-          pb[4 + e] = (__bf16)pw[NT - 1][e];
+          pb[i][e] = (__bf16)z[i][0][e];
+          pb[i][4 + e] = (__bf16)z[i][NT - 1][e];
         }
 #pragma unroll
-        for (int j = 0; j < W::kVec; ++j) {
-          const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
-          uint4 a;
-          a.x = __builtin_amdgcn_perm(vr[0][1][0][j / 2], vr[0][0][0][j / 2], sel);
-          a.y = __builtin_amdgcn_perm(vr[0][3][0][j / 2], vr[0][2][0][j / 2], sel);
-          a.z = __builtin_amdgcn_perm(vr[NT - 1][1][0][j / 2], vr[NT - 1][0][0][j / 2], sel);
-          a.w = __builtin_amdgcn_perm(vr[NT - 1][3][0][j / 2], vr[NT - 1][2][0][j / 2], sel);
-          o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), pb, o[i][j],
+      for (int j = 0; j < W::kVec; ++j) {
+        const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+        uint4 a;
+        a.x = __builtin_amdgcn_perm(vr[0][1][0][j / 2], vr[0][0][0][j / 2], sel);
+        a.y = __builtin_amdgcn_perm(vr[0][3][0][j / 2], vr[0][2][0][j / 2], sel);
+        a.z = __builtin_amdgcn_perm(vr[NT - 1][1][0][j / 2], vr[NT - 1][0][0][j / 2], sel);
+        a.w = __builtin_amdgcn_perm(vr[NT - 1][3][0][j / 2], vr[NT - 1][2][0][j / 2], sel);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), pb[i], o[i][j],
                                                             0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int b = 0; b < NL; ++b)
-#pragma unroll
-          for (int j = 0; j < W::kVec; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              o[i][b * W::kVec + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                  __uint_as_float(vr[0][e][b][j]), pw[0][e], o[i][b * W::kVec + j], 0, 0, 0);
       }
-      if constexpr (DRAFT) {
-        for (int t = 0; t < NT; ++t)
-          for (int e = 0; e < 4; ++e) {
-            if (bad[t][e] == 0) continue;
-            for (int x = 0; x < 4; ++x) {
-              if ((bad[t][e] >> (16 * x) & 0xFFFF) == 0) continue;
-              const int j = 16 * t + 4 * x + e;
-              // a constant index per trip of the unrolled loops would keep pw in registers;
-              // this path is rare enough for a select
-              float mine = 0.0f;
+    } else {
+#pragma unroll
+      for (int b = 0; b < NL; ++b)
+#pragma unroll
+        for (int j = 0; j < W::kVec; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+              o[i][b * W::kVec + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                  __uint_as_float(vr[0][e][b][j]), z[i][0][e], o[i][b * W::kVec + j], 0, 0, 0);
+    }
+    fetch_v();
+    if constexpr (DRAFT) {
+      for (int t = 0; t < NT; ++t)
+        for (int e = 0; e < 4; ++e) {
+          if (bad[t][e] == 0) continue;
+          for (int x = 0; x < 4; ++x) {
+            if ((bad[t][e] >> (16 * x) & 0xFFFF) == 0) continue;
+            const int j = 16 * t + 4 * x + e;
+            const T* src = vdb + (r0 + j) * at.dvr;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              float w = 0.0f;  // selected, not indexed: the weights stay in registers
 #pragma unroll
               for (int t2 = 0; t2 < NT; ++t2)
 #pragma unroll
-                for (int e2 = 0; e2 < 4; ++e2) mine = t2 == t && e2 == e ? pw[t2][e2] : mine;
-              const float w = __shfl(mine, 16 * x + m);
-              if (mask[i] >> j & 1) {
-                const T* src = vdb + (r0 + j) * at.dvr;
+                for (int e2 = 0; e2 < 4; ++e2) w = t2 == t && e2 == e ? z[i][t2][e2] : w;
+              w = __shfl(w, 16 * x + m);
+              if (!(mask[i] >> j & 1)) continue;
 #pragma unroll
-                for (int b = 0; b < NL; ++b)
+              for (int b = 0; b < NL; ++b)
 #pragma unroll
-                  for (int jj = 0; jj < W::kVec; ++jj)
+                for (int jj = 0; jj < W::kVec; ++jj)
 #pragma unroll
-                    for (int e2 = 0; e2 < 4; ++e2) {
-                      const T y = src[(16 * b + 4 * qg + e2) * W::kVec + jj];
-                      float val;
-                      if constexpr (W::kBf16) val = (float)y;
-                      else val = y;
-                      o[i][b * W::kVec + jj][e2] += w * val;
-                    }
-              }
+                  for (int e2 = 0; e2 < 4; ++e2)
+                    o[i][b * W::kVec + jj][e2] +=
+                        w * (float)src[(16 * b + 4 * qg + e2) * W::kVec + jj];
             }
           }
-      }
+        }
     }
   };
 
   const uint32_t none[MT] = {};
   const int csteps = (t1 - t0 + W::kStep - 1) / W::kStep;
-  for (int s = wave; s < csteps; s += 4) {
-    const int r0 = t0 + s * W::kStep;
-    load(kb, vb, g.kst, g.vst, r0, t1);
-    uint32_t seen = 0;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = r0 + 16 * t + 4 * qg + e;
-        bool see = j < t1;
-        if (accb) see = see && !(accb[min(j, t1 - 1)] < 0.0f);
-        seen |= (uint32_t)see << (4 * t + e);
-      }
-    step(std::false_type{}, seen, none, r0);
+  if (wave < csteps) {
+    // The next step's K is requested as soon as this one's has been multiplied, V
+    // likewise, into the same registers: a step's loads are in flight all the time.
+    int r0 = t0 + wave * W::kStep;
+    load_k(kb, g.kst, r0, t1);
+    float a = accb ? load_acc(r0, t1) : 0.0f;
+    load_v(vb, g.vst, r0, t1);
+    for (; r0 < t1; r0 += 4 * W::kStep) {
+      const int next = r0 + 4 * W::kStep, rows = min(W::kStep, t1 - r0);
+      uint32_t vis = rows == 32 ? ~0u : (1u << rows) - 1;
+      if (accb) vis &= ~(uint32_t)__ballot(a < 0.0f);
+      step(std::false_type{}, vis, none, r0,
+           [&] {
+             load_k(kb, g.kst, next, t1);
+             if (accb) a = load_acc(next, t1);
+           },
+           [&] { load_v(vb, g.vst, next, t1); });
+    }
   }
   if (drafts) {
     const int dsteps = (S + W::kStep - 1) / W::kStep;
     for (int s = (wave + 4 - (csteps & 3)) & 3; s < dsteps; s += 4) {
       const int r0 = s * W::kStep;
-      load(kdb, vdb, at.dkr, at.dvr, r0, S);
-      uint32_t seen = 0, mask[MT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) seen |= (uint32_t)(r0 + 16 * t + 4 * qg + e < S) << (4 * t + e);
+      load_k(kdb, at.dkr, r0, S);
+      load_v(vdb, at.dvr, r0, S);
+      const int rows = min(W::kStep, S - r0);
+      uint32_t mask[MT];
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         mask[i] = 0u;
@@ -309,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geo g, Attn at, Attend
           }
         }
       }
-      step(std::true_type{}, seen, mask, r0);
+      step(std::true_type{}, rows == 32 ? ~0u : (1u << rows) - 1, mask, r0, [] {}, [] {});
     }
   }
 
@@ -392,8 +417,11 @@ static hipError_t attend_typed(const AttnLaunch& A, const AttendSpace& w, const 
                   w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, ws_ptr<uint32_t>(ws, 0)};
   const int64_t pairs = (int64_t)g.U * w.splits;
   const int64_t grid = w.row_blocks > 1 ? (pairs + 7) / 8 * 8 * w.row_blocks : pairs;
-  attend_kernel<T, D, 1><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, w.chunk,
-                                                                         w.splits, w.row_blocks);
+  auto go = [&](auto kern) {
+    kern<<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, w.chunk, w.splits, w.row_blocks);
+  };
+  if (w.mt == 1) go(attend_kernel<T, D, 1>);
+  else go(attend_kernel<T, D, 2>);
   return hipGetLastError();
 }
 
@@ -501,16 +529,32 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     }
   }
   __syncthreads();
-  const int64_t tr = token_row(g, un);
-  const float* z = p.z + (((int64_t)un.l * g.H + un.h) * R) * g.T + un.t0;
-  for (int t = t0 + tid; t < min(un.n, t0 + kJoinTokens); t += kThreads) {
-    const float old = p.acc[tr + t];
-    if (old < 0.0f) continue;
-    float sum = 0.0f;
-    for (int r = 0; r < R; ++r)
-      if (sw[r] != 0.0f) sum = __builtin_fmaf(sw[r], exp2_fast(z[r * g.T + t] - slse[r]), sum);
-    p.acc[tr + t] = at.decay > 0.0f ? __builtin_fmaf(at.decay, old, sum) : sum;
+  const int64_t tr = token_row(g, un) + t0;
+  const float* z = p.z + (((int64_t)un.l * g.H + un.h) * R) * g.T + un.t0 + t0;
+  const int left = un.n - t0;
+  constexpr int PER = kJoinTokens / kThreads;
+  float old[PER], sum[PER];
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    old[x] = tid + x * kThreads < left ? p.acc[tr + tid + x * kThreads] : -1.0f;
+    sum[x] = 0.0f;
   }
+#pragma unroll 4
+  for (int r = 0; r < R; ++r) {
+    const float w = sw[r], ls = slse[r];
+    float y[PER];
+#pragma unroll
+    for (int x = 0; x < PER; ++x)
+      y[x] = tid + x * kThreads < left ? z[r * g.T + tid + x * kThreads] : -INFINITY;
+    if (w != 0.0f)
+#pragma unroll
+      for (int x = 0; x < PER; ++x) sum[x] = __builtin_fmaf(w, exp2_fast(y[x] - ls), sum[x]);
+  }
+#pragma unroll
+  for (int x = 0; x < PER; ++x)
+    if (tid + x * kThreads < left && !(old[x] < 0.0f))
+      p.acc[tr + tid + x * kThreads] =
+          at.decay > 0.0f ? __builtin_fmaf(at.decay, old[x], sum[x]) : sum[x];
   if (blk == 0 && p.acc_draft && tid < S) {
     float sum = 0.0f;
     for (int r = 0; r < R; ++r)
