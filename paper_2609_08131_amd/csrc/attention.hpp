@@ -89,18 +89,18 @@ __device__ __forceinline__ f32x4 logits(const uint4 (&k)[Row<T, D>::kPieces],
   return z;
 }
 
-// Query row r of a unit's R rows (pieces of lane group qg); zeros past the last row.
+// Query row r of a unit's rows (pieces of lane group qg), zeros where it is not
+// used; r < R in any case. No branch: one on the lane's row would take the
+// unit's addresses out of the scalar registers.
 template <typename T, int D>
-__device__ __forceinline__ void load_row(const Geo& g, const T* qu, int r, int R, int qg,
+__device__ __forceinline__ void load_row(const Geo& g, const T* qu, int r, bool used, int qg,
                                          uint4 (&f)[Row<T, D>::kPieces]) {
-  if (r < R) {
-    const int head = r / g.w, p = r - head * g.w;
-    const char* src = reinterpret_cast<const char*>(qu + head * g.qsh + p * g.qsp) + 16 * qg;
+  const int head = r / g.w, p = r - head * g.w;
+  const char* src = reinterpret_cast<const char*>(qu + head * g.qsh + p * g.qsp) + 16 * qg;
 #pragma unroll
-    for (int a = 0; a < Row<T, D>::kPieces; ++a) f[a] = *reinterpret_cast<const uint4*>(src + 64 * a);
-  } else {
-#pragma unroll
-    for (int a = 0; a < Row<T, D>::kPieces; ++a) f[a] = uint4{0, 0, 0, 0};
+  for (int a = 0; a < Row<T, D>::kPieces; ++a) {
+    const uint4 x = *reinterpret_cast<const uint4*>(src + 64 * a);
+    f[a] = used ? x : uint4{0, 0, 0, 0};
   }
 }
 

@@ -112,10 +112,18 @@ __device__ __forceinline__ bool live_ok(const Geo& g, int b, int n) {
 }
 
 // decode_unit with n = the sequence's current length (0 where it contradicts
-// the offsets), for the kernels whose caller may give lengths of their own.
+// the offsets), for the kernels whose caller may give lengths of their own. The
+// unit is the workgroup's: what names its rows is kept in scalar registers, where the
+// buffer descriptors made from it belong (from vector registers every load
+// would become a loop over the lanes' descriptors).
 __device__ __forceinline__ Unit live_unit(const Geo& g, int u) {
   Unit r = decode_unit(g, u);
   if (g.live) r.n = live_ok(g, r.b, r.n) ? g.live[r.b] : 0;
+  r.b = __builtin_amdgcn_readfirstlane(r.b);
+  r.l = __builtin_amdgcn_readfirstlane(r.l);
+  r.h = __builtin_amdgcn_readfirstlane(r.h);
+  r.t0 = __builtin_amdgcn_readfirstlane((int)r.t0);
+  r.n = __builtin_amdgcn_readfirstlane(r.n);
   return r;
 }
 

@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     row[i] = (rb * MT + i) * 16 + m;
-    load_row<T, D>(g, unit_queries(g, un, p.q), row[i], R, qg, qf[i]);
+    load_row<T, D>(g, unit_queries(g, un, p.q), min(row[i], R - 1), row[i] < R, qg, qf[i]);
   }
 
   f32x4 o[MT][W::kBlocks];
@@ -93,9 +93,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
 
   const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
   const T* vb = p.v + un.l * g.vsl + un.h * g.vsh + un.t0 * g.vst;
-  const T* kdb = p.kd + un.b * at.dks + un.l * at.dkl + un.h * at.dkh;
-  const T* vdb = p.vd + un.b * at.dvs + un.l * at.dvl + un.h * at.dvh;
-  const float* accb = p.acc ? p.acc + token_row(g, un) : nullptr;
+  const bool hides = p.acc != nullptr;
+  const float* accb = p.acc + token_row(g, un);  // read only where p.acc is given
 
   uint4 kf[NT][NP];
   uint32_t vr[NT][4][NL][VW];
@@ -267,7 +266,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
           for (int x = 0; x < 4; ++x) {
             if ((bad[t][e] >> (16 * x) & 0xFFFF) == 0) continue;
             const int j = 16 * t + 4 * x + e;
-            const T* src = vdb + (r0 + j) * at.dvr;
+            const T* src = p.vd + un.b * at.dvs + un.l * at.dvl + un.h * at.dvh + (r0 + j) * at.dvr;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
               float w = 0.0f;  // selected, not indexed: the weights stay in registers
@@ -298,21 +297,24 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     // likewise, into the same registers: a step's loads are in flight all the time.
     int r0 = t0 + wave * W::kStep;
     load_k(kb, g.kst, r0, t1);
-    float a = accb ? load_acc(r0, t1) : 0.0f;
+    float a = 0.0f;
+    if (hides) a = load_acc(r0, t1);
     load_v(vb, g.vst, r0, t1);
     for (; r0 < t1; r0 += 4 * W::kStep) {
       const int next = r0 + 4 * W::kStep, rows = min(W::kStep, t1 - r0);
       uint32_t vis = rows == 32 ? ~0u : (1u << rows) - 1;
-      if (accb) vis &= ~(uint32_t)__ballot(a < 0.0f);
+      if (hides) vis &= ~(uint32_t)__ballot(a < 0.0f);
       step(std::false_type{}, vis, none, r0,
            [&] {
              load_k(kb, g.kst, next, t1);
-             if (accb) a = load_acc(next, t1);
+             if (hides) a = load_acc(next, t1);
            },
            [&] { load_v(vb, g.vst, next, t1); });
     }
   }
   if (drafts) {
+    const T* kdb = p.kd + un.b * at.dks + un.l * at.dkl + un.h * at.dkh;
+    const T* vdb = p.vd + un.b * at.dvs + un.l * at.dvl + un.h * at.dvh;
     const int dsteps = (S + W::kStep - 1) / W::kStep;
     for (int s = (wave + 4 - (csteps & 3)) & 3; s < dsteps; s += 4) {
       const int r0 = s * W::kStep;

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(kThreads) void attn_lse_kernel(Geo g, Attn at, LseA
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int r = rr0 + 16 * i + m;
-      load_row<T, D>(g, unit_queries(g, un, p.q), r, R, qg, qf[i]);
+      load_row<T, D>(g, unit_queries(g, un, p.q), min(r, R - 1), r < R, qg, qf[i]);
       last[i] = at.causal ? first + r % w : INT32_MAX;
     }
     const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumA
       ls = lseu[r];
     }
     const bool live = rw != 0.0f && ls != -INFINITY;
-    load_row<T, D>(g, qu, live ? r : R, R, qg, qf);
+    load_row<T, D>(g, qu, min(r, R - 1), live, qg, qf);
     // Rows that add nothing: a masked tile, where their weights are set to 0.
     const int last = !live ? -1 : causal ? first + pos : INT32_MAX;
     const bool masked = DRAFT || __ballot(last < tok + 16 * NT) != 0;
