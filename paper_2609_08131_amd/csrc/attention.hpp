@@ -70,6 +70,12 @@ struct Row {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// 16 bytes to byte offset `off` of a buffer range; nothing past its end.
+__device__ __forceinline__ void buffer_store16(__amdgpu_buffer_rsrc_t r, int32_t off, f32x4 x) {
+  typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4v, x), r, off, 0, 0);
+}
+
 // The 16 x 16 logits tile of 16 tokens and 16 query rows.
 template <typename T, int D>
 __device__ __forceinline__ f32x4 logits(const uint4 (&k)[Row<T, D>::kPieces],
@@ -137,7 +143,7 @@ struct AttendSpace {
   size_t ml;           // float2 [U][R][splits]     (maximum, sum) of a chunk
   size_t part;         // float  [U][R][splits][D]  its unnormalised output
   size_t lse;          // float  [U][R]
-  size_t z;            // float  [L][H][R][T]       kept logits (accumulating from few rows)
+  size_t z;            // float  [L][H][tiles][R][16] kept logits (accumulating from few rows)
   size_t zd;           // float  [U][R][S]          ... and the drafted tokens'
   size_t total;
   bool keep;           // logits are kept

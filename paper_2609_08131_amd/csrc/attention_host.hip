@@ -137,7 +137,7 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   w->part = o;
   if (w->splits > 1) o = align256(o + 4 * (size_t)UR * w->splits * g.D);
   w->z = o;
-  if (w->keep) o = align256(o + 4 * (size_t)LHT * A.at.R);
+  if (w->keep) o = align256(o + 4 * (size_t)g.L * g.H * (g.T / 16 + g.B + 1) * 16 * A.at.R);
   w->zd = o;
   if (w->keep) o = align256(o + 4 * (size_t)UR * g.w);
   *sum = WeightsSpace{};

@@ -369,17 +369,17 @@ __device__ __forceinline__ f64x4 mfma64(double a, double b, f64x4 acc) {
 }
 
 // WORDS consecutive 32-bit words at byte offset `off` of a buffer range.
-template <int WORDS>
+template <int WORDS, int POLICY = 0>
 __device__ __forceinline__ void buffer_load_words(__amdgpu_buffer_rsrc_t r, int32_t off,
                                                   uint32_t (&x)[WORDS]) {
   static_assert(WORDS == 2 || WORDS % 4 == 0, "8- or 16-byte loads");
   if constexpr (WORDS == 2) {
-    const auto y = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+    const auto y = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, POLICY);
     x[0] = y[0]; x[1] = y[1];
   } else {
 #pragma unroll
     for (int i = 0; i < WORDS / 4; ++i) {
-      const uint4 y = buffer_load16(r, off + 16 * i);
+      const uint4 y = buffer_load16<POLICY>(r, off + 16 * i);
       x[4 * i] = y.x; x[4 * i + 1] = y.y; x[4 * i + 2] = y.z; x[4 * i + 3] = y.w;
     }
   }

@@ -43,10 +43,19 @@ struct AttendArgs {
 // rescale the output; the weights stay below 2^8, far inside fp32 and bf16.
 constexpr float kLazyMax = 8.0f;
 
-// Four floats at a 4-byte aligned address.
-struct __attribute__((packed, aligned(4))) Float4 { float x, y, z, w; };
+// What the accumulators do in a call, apart in the code: a load or store that
+// only some calls make would have the others' waits count it too.
+enum Mode { kPlain, kHides, kKeeps };  // not read; hide empty slots; and the logits are kept
 
-template <typename T, int D, int MT>
+// Kept logits lie by 16-token tiles, [R][16] each. A sequence's tiles start behind
+// t0 / 16 + b others of its (layer, KV head) row, which leaves room for every
+// sequence's last, partial tile.
+__host__ __device__ __forceinline__ int64_t keep_tiles(const Geo& g) { return g.T / 16 + g.B + 1; }
+__device__ __forceinline__ int64_t keep_at(const Geo& g, const Unit& un, int R, int tile) {
+  return ((((int64_t)un.l * g.H + un.h) * keep_tiles(g)) + un.t0 / 16 + un.b + tile) * R * 16;
+}
+
+template <typename T, int D, int MT, Mode MODE>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, AttendArgs<T> p,
                                                           int chunk, int splits, int row_blocks) {
   using W = Row<T, D>;
@@ -93,11 +102,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
 
   const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
   const T* vb = p.v + un.l * g.vsl + un.h * g.vsh + un.t0 * g.vst;
-  const bool hides = p.acc != nullptr;
-  const float* accb = p.acc + token_row(g, un);  // read only where p.acc is given
+  constexpr bool HIDES = MODE != kPlain;
+  const float* accb = p.acc + token_row(g, un);  // read only where the call hides
 
   uint4 kf[NT][NP];
   uint32_t vr[NT][4][NL][VW];
+  // V is read in whole lines, once where the rows are one block: streamed past the
+  // caches (a token over 8 layers of 131072: 6.2 TB/s without the hint, 6.9 with it).
+  // K's loads take half lines and keep the default policy.
+  constexpr int kVPolicy = MT == 1 ? kPolicyStream : kPolicyShared;
   // Rows [r0, end) of a K or V row range, at most a step of them (zeros past the end).
   auto load_k = [&](const T* base, int64_t stride, int r0, int end) {
     const int32_t bytes = (int32_t)(stride * sizeof(T));
@@ -118,7 +131,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int b = 0; b < NL; ++b)
-          buffer_load_words(rs, (16 * t + 4 * qg + i) * bytes + (16 * b + m) * W::kVBytes, vr[t][i][b]);
+          buffer_load_words<VW, kVPolicy>(rs, (16 * t + 4 * qg + i) * bytes + (16 * b + m) * W::kVBytes,
+                                          vr[t][i][b]);
   };
   // The accumulator entry of token r0 + lane % kStep (0 past the end): one load per
   // step; a ballot of their signs is the step's hidden tokens.
@@ -178,21 +192,25 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
           }
         }
     }
-    if (MT == 1 && p.z != nullptr && row[0] < R) {
-      // kept for the accumulation, in powers of two
-      const int end = (DRAFT ? S : t1) - r0;
-      float* dst = (DRAFT ? p.zd + ((int64_t)u * R + row[0]) * S
-                          : p.z + (((int64_t)un.l * g.H + un.h) * R + row[0]) * g.T + un.t0) + r0;
+    if constexpr (MODE == kKeeps) {
+      // in powers of two, for the accumulation
+      if constexpr (DRAFT) {
+        float* dst = p.zd + ((int64_t)u * R + min(row[0], R - 1)) * S + r0;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int j = 16 * t + 4 * qg;
-        if (j + 4 <= end) {
-          *reinterpret_cast<Float4*>(dst + j) =
-              Float4{z[0][t][0] * at.c, z[0][t][1] * at.c, z[0][t][2] * at.c, z[0][t][3] * at.c};
-        } else {
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (j + e < end) dst[j + e] = z[0][t][e] * at.c;
+            if (row[0] < R && r0 + 16 * t + 4 * qg + e < S) dst[16 * t + 4 * qg + e] = z[0][t][e] * at.c;
+      } else {
+        // (the chunk's last step may have no second tile: its room is another's)
+        const auto rs = buffer_range(p.z + keep_at(g, un, R, r0 / 16),
+                                     min(NT, (t1 - r0 + 15) / 16) * R * 64);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = z[0][t][e] * at.c;
+          buffer_store16(rs, row[0] < R ? t * R * 64 + row[0] * 64 + qg * 16 : NT * kKeepRows * 64, x);
         }
       }
     }
@@ -298,16 +316,16 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     int r0 = t0 + wave * W::kStep;
     load_k(kb, g.kst, r0, t1);
     float a = 0.0f;
-    if (hides) a = load_acc(r0, t1);
+    if constexpr (HIDES) a = load_acc(r0, t1);
     load_v(vb, g.vst, r0, t1);
     for (; r0 < t1; r0 += 4 * W::kStep) {
       const int next = r0 + 4 * W::kStep, rows = min(W::kStep, t1 - r0);
       uint32_t vis = rows == 32 ? ~0u : (1u << rows) - 1;
-      if (hides) vis &= ~(uint32_t)__ballot(a < 0.0f);
+      if constexpr (HIDES) vis &= ~(uint32_t)__ballot(a < 0.0f);
       step(std::false_type{}, vis, none, r0,
            [&] {
              load_k(kb, g.kst, next, t1);
-             if (hides) a = load_acc(next, t1);
+             if constexpr (HIDES) a = load_acc(next, t1);
            },
            [&] { load_v(vb, g.vst, next, t1); });
     }
@@ -387,7 +405,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     }
     if (r < R) {
       const int64_t ur = (int64_t)u * R + r;
-      if ((tid & 15) == 0 && (splits > 1 || p.z)) p.ml[ur * splits + split] = float2{jt, sum};
+      if ((tid & 15) == 0 && (splits > 1 || MODE == kKeeps)) p.ml[ur * splits + split] = float2{jt, sum};
       if (nsp == 1) {
         const int head = r / S, pos = r - head * S;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -422,8 +440,11 @@ static hipError_t attend_typed(const AttnLaunch& A, const AttendSpace& w, const 
   auto go = [&](auto kern) {
     kern<<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, w.chunk, w.splits, w.row_blocks);
   };
-  if (w.mt == 1) go(attend_kernel<T, D, 1>);
-  else go(attend_kernel<T, D, 2>);
+  if (w.keep) go(attend_kernel<T, D, 1, kKeeps>);
+  else if (w.mt == 1 && acc) go(attend_kernel<T, D, 1, kHides>);
+  else if (w.mt == 1) go(attend_kernel<T, D, 1, kPlain>);
+  else if (acc) go(attend_kernel<T, D, 2, kHides>);
+  else go(attend_kernel<T, D, 2, kPlain>);
   return hipGetLastError();
 }
 
@@ -532,7 +553,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   }
   __syncthreads();
   const int64_t tr = token_row(g, un) + t0;
-  const float* z = p.z + (((int64_t)un.l * g.H + un.h) * R) * g.T + un.t0 + t0;
+  // token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x
+  const float* z = p.z + keep_at(g, un, R, t0 / 16 + tid / 16) + tid % 16;
   const int left = un.n - t0;
   constexpr int PER = kJoinTokens / kThreads;
   float old[PER], sum[PER];
@@ -547,7 +569,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     float y[PER];
 #pragma unroll
     for (int x = 0; x < PER; ++x)
-      y[x] = tid + x * kThreads < left ? z[r * g.T + tid + x * kThreads] : -INFINITY;
+      y[x] = tid + x * kThreads < left ? z[x * (kThreads / 16) * R * 16 + r * 16] : -INFINITY;
     if (w != 0.0f)
 #pragma unroll
       for (int x = 0; x < PER; ++x) sum[x] = __builtin_fmaf(w, exp2_fast(y[x] - ls), sum[x]);
