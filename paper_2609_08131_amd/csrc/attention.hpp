@@ -24,7 +24,7 @@ constexpr int kMaxDraft = 512;        // rows per query head jacap_attend takes
 constexpr int kKeepRows = 16;
 constexpr int kAttendChunk = 8192;    // tokens per workgroup of the attention: at most,
 constexpr int kAttendChunkMin = 256;  // ... and at least
-constexpr int kAttendBlocks = 1024;   // chunks shrink until the grid has this many workgroups
+constexpr int kAttendBlocks = 512;   // chunks shrink until the grid has this many workgroups
 constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
 // The log-sum pass: 16-row tiles per workgroup (their queries in registers),
 // tokens per workgroup.

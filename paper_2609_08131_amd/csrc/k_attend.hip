@@ -134,12 +134,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
           buffer_load_words<VW, kVPolicy>(rs, (16 * t + 4 * qg + i) * bytes + (16 * b + m) * W::kVBytes,
                                           vr[t][i][b]);
   };
-  // The accumulator entry of token r0 + lane % kStep (0 past the end): one load per
-  // step; a ballot of their signs is the step's hidden tokens.
-  auto load_acc = [&](int r0, int end) {
-    return buffer_load_f32(buffer_range(accb + r0, 4 * max(0, min(W::kStep, end - r0))),
-                           4 * (lane & (W::kStep - 1)));
+  // The accumulator entry of token r0 + lane % kStep (0 past the chunk's end): one load
+  // per step; a ballot of their signs is the step's hidden tokens.
+  const auto acc_range = buffer_range(accb + t0, 4 * max(0, t1 - t0));
+  auto load_acc = [&](int r0) {
+    return buffer_load_f32(acc_range, 4 * (r0 - t0 + (lane & (W::kStep - 1))));
   };
+  // The chunk's kept logits: its own tiles (its last step may have no second one, whose
+  // room would be another's).
+  const auto keep_range = buffer_range(p.z + keep_at(g, un, R, t0 / 16), (t1 - t0 + 15) / 16 * R * 64);
 
   // One step over the K and V rows held. vis: bit j, token j of the step is one that rows
   // may see; DRAFT: each row sees those of its mask only. `fetch_k` and
@@ -202,15 +205,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
           for (int e = 0; e < 4; ++e)
             if (row[0] < R && r0 + 16 * t + 4 * qg + e < S) dst[16 * t + 4 * qg + e] = z[0][t][e] * at.c;
       } else {
-        // (the chunk's last step may have no second tile: its room is another's)
-        const auto rs = buffer_range(p.z + keep_at(g, un, R, r0 / 16),
-                                     min(NT, (t1 - r0 + 15) / 16) * R * 64);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           f32x4 x;
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[e] = z[0][t][e] * at.c;
-          buffer_store16(rs, row[0] < R ? t * R * 64 + row[0] * 64 + qg * 16 : NT * kKeepRows * 64, x);
+          buffer_store16(keep_range,
+                         row[0] < R ? (((r0 - t0) / 16 + t) * R + row[0]) * 64 + qg * 16 : INT32_MAX - 15, x);
         }
       }
     }
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     int r0 = t0 + wave * W::kStep;
     load_k(kb, g.kst, r0, t1);
     float a = 0.0f;
-    if constexpr (HIDES) a = load_acc(r0, t1);
+    if constexpr (HIDES) a = load_acc(r0);
     load_v(vb, g.vst, r0, t1);
     for (; r0 < t1; r0 += 4 * W::kStep) {
       const int next = r0 + 4 * W::kStep, rows = min(W::kStep, t1 - r0);
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
       step(std::false_type{}, vis, none, r0,
            [&] {
              load_k(kb, g.kst, next, t1);
-             if constexpr (HIDES) a = load_acc(next, t1);
+             if constexpr (HIDES) a = load_acc(next);
            },
            [&] { load_v(vb, g.vst, next, t1); });
     }
@@ -531,19 +532,42 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   const int t0 = blk * kJoinTokens;
   if (t0 >= un.n && blk > 0) return;
   const int nsp = max(1, (un.n + chunk - 1) / chunk);
+  // The entries and the first rows' logits are requested before the rows' lse is
+  // joined. Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
+  const int64_t tr = token_row(g, un) + t0;
+  const float* z = p.z + keep_at(g, un, R, t0 / 16 + tid / 16) + tid % 16;
+  const int left = un.n - t0;
+  constexpr int PER = kJoinTokens / kThreads, FIRST = 4;
+  float old[PER], sum[PER], y[FIRST][PER];
+  auto logit = [&](int r, int x) {
+    return tid + x * kThreads < left ? z[x * (kThreads / 16) * R * 16 + r * 16] : -INFINITY;
+  };
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    old[x] = tid + x * kThreads < left ? p.acc[tr + tid + x * kThreads] : -1.0f;
+    sum[x] = 0.0f;
+#pragma unroll
+    for (int r = 0; r < FIRST; ++r) y[r][x] = r < R ? logit(r, x) : -INFINITY;
+  }
   __shared__ float slse[kKeepRows], sw[kKeepRows];
   {
     // 16 threads per row
     const int r = tid >> 4;
     float top = -INFINITY, l = 0.0f;
     const float2* ml = p.ml + ((int64_t)u * R + min(r, R - 1)) * splits;
-    for (int s = tid & 15; s < nsp; s += 16) top = fmaxf(top, ml[s].x);
+    for (int s = tid & 15; s < nsp; s += 16) {
+      const float2 c = ml[s];
+      const float now = fmaxf(top, c.x), ref = finite_ref(now);
+      l = l * exp2_fast(top - ref) + c.y * exp2_fast(c.x - ref);
+      top = now;
+    }
 #pragma unroll
-    for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    const float ref = finite_ref(top);
-    for (int s = tid & 15; s < nsp; s += 16) l += ml[s].y * exp2_fast(ml[s].x - ref);
-#pragma unroll
-    for (int x = 8; x > 0; x >>= 1) l += __shfl_xor(l, x);
+    for (int x = 8; x > 0; x >>= 1) {
+      const float t = __shfl_xor(top, x), m = __shfl_xor(l, x);
+      const float now = fmaxf(top, t), ref = finite_ref(now);
+      l = l * exp2_fast(top - ref) + m * exp2_fast(t - ref);
+      top = now;
+    }
     if ((tid & 15) == 0) {
       float w = 0.0f;
       if (r < R && l != 0.0f) w = at.row_weight ? at.row_weight[(int64_t)un.b * S + r % S] : 1.0f;
@@ -552,27 +576,21 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     }
   }
   __syncthreads();
-  const int64_t tr = token_row(g, un) + t0;
-  // token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x
-  const float* z = p.z + keep_at(g, un, R, t0 / 16 + tid / 16) + tid % 16;
-  const int left = un.n - t0;
-  constexpr int PER = kJoinTokens / kThreads;
-  float old[PER], sum[PER];
-#pragma unroll
-  for (int x = 0; x < PER; ++x) {
-    old[x] = tid + x * kThreads < left ? p.acc[tr + tid + x * kThreads] : -1.0f;
-    sum[x] = 0.0f;
-  }
-#pragma unroll 4
-  for (int r = 0; r < R; ++r) {
+  auto add = [&](int r, const float (&v)[PER]) {
     const float w = sw[r], ls = slse[r];
-    float y[PER];
-#pragma unroll
-    for (int x = 0; x < PER; ++x)
-      y[x] = tid + x * kThreads < left ? z[x * (kThreads / 16) * R * 16 + r * 16] : -INFINITY;
     if (w != 0.0f)
 #pragma unroll
-      for (int x = 0; x < PER; ++x) sum[x] = __builtin_fmaf(w, exp2_fast(y[x] - ls), sum[x]);
+      for (int x = 0; x < PER; ++x) sum[x] = __builtin_fmaf(w, exp2_fast(v[x] - ls), sum[x]);
+  };
+#pragma unroll
+  for (int r = 0; r < FIRST; ++r)
+    if (r < R) add(r, y[r]);
+#pragma unroll 4
+  for (int r = FIRST; r < R; ++r) {
+    float v[PER];
+#pragma unroll
+    for (int x = 0; x < PER; ++x) v[x] = logit(r, x);
+    add(r, v);
   }
 #pragma unroll
   for (int x = 0; x < PER; ++x)
