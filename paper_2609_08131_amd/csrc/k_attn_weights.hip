@@ -71,23 +71,31 @@ __global__ __launch_bounds__(kThreads) void attn_lse_kernel(Geo g, Attn at, LseA
       last[i] = at.causal ? first + r % w : INT32_MAX;
     }
     const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
-    const float* accb = p.acc + token_row(g, un);
     const int32_t ks = (int32_t)(g.kst * sizeof(T));
-    for (int r0 = t0 + 16 * wave; r0 < t1; r0 += 64) {
+    const auto acc_range = buffer_range(p.acc + token_row(g, un) + t0, 4 * (t1 - t0));
+    uint4 kf[NP];
+    float a;
+    // (zeros past the chunk's end)
+    auto load = [&](int r0) {
       const auto kr = buffer_range(kb + r0 * g.kst, rows_bytes(min(16, t1 - r0), ks, W::kBytes));
-      uint4 kf[NP];
 #pragma unroll
-      for (int a = 0; a < NP; ++a) kf[a] = buffer_load16(kr, m * ks + 64 * a + 16 * qg);
-      uint32_t seen = 0;
+      for (int x = 0; x < NP; ++x) kf[x] = buffer_load16(kr, m * ks + 64 * x + 16 * qg);
+      a = buffer_load_f32(acc_range, 4 * (r0 - t0 + m));
+    };
+    load(t0 + 16 * wave);
+    for (int r0 = t0 + 16 * wave; r0 < t1; r0 += 64) {
+      // the next step's keys are requested before this one is multiplied
+      uint4 kc[NP];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = r0 + 4 * qg + e;
-        seen |= (uint32_t)(j < t1 && !(accb[min(j, t1 - 1)] < 0.0f)) << e;
-      }
-      const bool masked = r0 + 16 > all || __ballot(seen != 15u) != 0;
+      for (int x = 0; x < NP; ++x) kc[x] = kf[x];
+      const int rows = min(16, t1 - r0);
+      const uint32_t vis = ((1u << rows) - 1) & ~(uint32_t)__ballot(a < 0.0f);
+      load(r0 + 64);
+      const bool masked = r0 + 16 > all || (vis & 0xFFFF) != 0xFFFF;
+      const uint32_t seen = vis >> (4 * qg);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        f32x4 z = logits<T, D>(kf, qf[i]);
+        f32x4 z = logits<T, D>(kc, qf[i]);
         if (masked) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -184,9 +192,13 @@ hipError_t launch_attn_lse(const AttnLaunch& A, const WeightsSpace& w, const voi
 
 // ---------------------------------------------------------------------------
 // Sums: a workgroup takes 64 NT tokens of a unit, 16 NT per wave with their keys in
-// registers, and a part of the rows, 16 at a time. A lane adds the weights its
+// registers, and a part of the rows, kStageRows at a time through LDS (two
+// buffers, the next rows requested a stage ahead). A lane adds the weights its
 // query row gives its tokens; the 16 lanes of a tile's rows are added at the
 // end. DRAFT: the tokens are the drafted ones, seen by the tree's mask.
+//
+// A staged row has 16 bytes of padding: the 16 lanes that read one piece of 16
+// rows then touch all banks.
 // ---------------------------------------------------------------------------
 template <typename T>
 struct SumArgs {
@@ -197,14 +209,19 @@ struct SumArgs {
   uint32_t* status;   // or null
 };
 
+constexpr int kStageRows = 32;
+
 template <typename T, int D, int NT, bool DRAFT>
 __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumArgs<T> p, int blocks,
                                                             int row_splits) {
   using W = Row<T, D>;
   constexpr int NP = W::kPieces;
+  constexpr int PITCH = W::kBytes + 16;
+  constexpr int SHARE = kStageRows * W::kBytes / 16 / kThreads;  // 16-byte pieces per thread and stage
+  constexpr int LANES = W::kBytes / 16 / SHARE;                  // threads per staged row
+  static_assert(LANES * kStageRows == kThreads, "a thread stages one row's pieces");
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (blockIdx.x == 0 && p.status) write_status(g, p.status);
   // row parts of a token block together; a causal prompt's first tokens, which
   // the most rows see, first
   int x = blockIdx.x;
@@ -213,106 +230,154 @@ __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumA
   const int u = x % g.U, blk = x / g.U;
   const Unit un = live_unit(g, u);
   const int n = DRAFT ? g.w : un.n;
-  const int tok = blk * 64 * NT + wave * 16 * NT;  // the wave's first token
-  if (tok >= n) return;
+  const int btok = blk * 64 * NT;            // the workgroup's first token
+  const int tok = btok + wave * 16 * NT;     // the wave's
   const int R = at.R, w = g.w;
   const bool causal = !DRAFT && at.causal;
   const int first = causal ? un.n - w : 0;
-
-  const int64_t kst = DRAFT ? at.dkr : g.kst;
-  const T* kb = DRAFT ? p.k + un.b * at.dks + un.l * at.dkl + un.h * at.dkh
-                      : p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
-  const int32_t ks = (int32_t)(kst * sizeof(T));
-  uint4 kf[NT][NP];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int r0 = tok + 16 * t;
-    const auto kr = buffer_range(kb + r0 * kst, rows_bytes(min(16, n - r0), ks, W::kBytes));
-#pragma unroll
-    for (int a = 0; a < NP; ++a) kf[t][a] = buffer_load16(kr, m * ks + 64 * a + 16 * qg);
-  }
-  const T* qu = unit_queries(g, un, p.q);
-  const float* lseu = p.lse + ((int64_t)un.b * g.L + un.l) * g.Hq * w + (int64_t)un.h * R;
-
-  f32x4 sum[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int tiles = (R + 15) / 16;
-  const int per = (tiles + row_splits - 1) / row_splits;
-  const int tile1 = min(tiles, (part + 1) * per);
-  for (int tile = part * per; tile < tile1; ++tile) {
-    if (causal) {
-      // rows of one head whose positions all lie before the wave's tokens see none
-      const int r0 = tile * 16, head = r0 / w, p0 = r0 - head * w;
-      if (p0 + 15 < w && first + p0 + 15 < tok) {
-        tile = max(tile, min((head * w + min(w, tok - first)) / 16, tile1) - 1);
-        continue;
-      }
+  const int stages = (R + kStageRows - 1) / kStageRows;
+  const int per = (stages + row_splits - 1) / row_splits;
+  const int stage1 = min(stages, (part + 1) * per);
+  // The first stage from s on with a row that sees the workgroup's tokens: whole
+  // stages of one head whose positions all lie before them are skipped.
+  auto useful = [&](int s) {
+    if (causal && s < stage1) {
+      const int r0 = s * kStageRows, head = r0 / w, p0 = r0 - head * w;
+      if (p0 + kStageRows <= w && first + p0 + kStageRows - 1 < btok)
+        s = (head * w + min(w, btok - first)) / kStageRows;
     }
-    const int r = tile * 16 + m;
-    const int head = r / w, pos = r - head * w;
-    uint4 qf[NP];
-    float rw = 0.0f, ls = INFINITY;
-    if (r < R) {
-      rw = at.row_weight ? at.row_weight[(int64_t)un.b * w + pos] : 1.0f;
-      ls = lseu[r];
-    }
-    const bool live = rw != 0.0f && ls != -INFINITY;
-    load_row<T, D>(g, qu, min(r, R - 1), live, qg, qf);
-    // Rows that add nothing: a masked tile, where their weights are set to 0.
-    const int last = !live ? -1 : causal ? first + pos : INT32_MAX;
-    const bool masked = DRAFT || __ballot(last < tok + 16 * NT) != 0;
-    ls *= kLog2e;
+    return s;
+  };
+
+  if (btok < n) {
+    const int64_t kst = DRAFT ? at.dkr : g.kst;
+    const T* kb = DRAFT ? p.k + un.b * at.dks + un.l * at.dkl + un.h * at.dkh
+                        : p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
+    const int32_t ks = (int32_t)(kst * sizeof(T));
+    uint4 kf[NT][NP];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const f32x4 z = logits<T, D>(kf[t], qf);
-      uint32_t bits = 0;
-      if constexpr (DRAFT) {
-        const int j0 = tok + 16 * t;
-        if (live && j0 < n) {
-          if (at.tree) bits = at.tree[((int64_t)un.b * w + pos) * at.tree_words + (j0 >> 5)] >> (j0 & 31);
-          else bits = pos < j0 ? 0u : pos - j0 >= 31 ? ~0u : (2u << (pos - j0)) - 1u;
+      const int r0 = tok + 16 * t;
+      const auto kr = buffer_range(kb + r0 * kst, rows_bytes(min(16, n - r0), ks, W::kBytes));
+#pragma unroll
+      for (int a = 0; a < NP; ++a) kf[t][a] = buffer_load16(kr, m * ks + 64 * a + 16 * qg);
+    }
+    const T* qu = unit_queries(g, un, p.q);
+    const float* lseu = p.lse + ((int64_t)un.b * g.L + un.l) * g.Hq * w + (int64_t)un.h * R;
+    const float* rwu = at.row_weight ? at.row_weight + (int64_t)un.b * w : nullptr;
+
+    __shared__ __align__(16) char rows_lds[2][kStageRows * PITCH];
+    struct Meta { float lse, weight; int last, pos; };  // last position seen, -1: adds nothing
+    __shared__ Meta meta[2][kStageRows];
+    const int srow = tid / LANES, spiece = tid % LANES * SHARE;
+    uint4 held[SHARE];
+    Meta mine;
+    auto fetch = [&](int s) {
+      const int r = min(s * kStageRows + srow, R - 1);
+      const int head = r / w, pos = r - head * w;
+      const char* src = reinterpret_cast<const char*>(qu + head * g.qsh + pos * g.qsp);
+#pragma unroll
+      for (int i = 0; i < SHARE; ++i) held[i] = *reinterpret_cast<const uint4*>(src + 16 * (spiece + i));
+      mine.lse = lseu[r];
+      mine.weight = rwu ? rwu[pos] : 1.0f;
+      mine.pos = pos;
+      mine.last = s * kStageRows + srow < R ? (causal ? first + pos : INT32_MAX) : -1;
+    };
+    auto store = [&](int buf) {
+      const bool live = mine.last >= 0 && mine.weight != 0.0f && mine.lse != -INFINITY;
+#pragma unroll
+      for (int i = 0; i < SHARE; ++i)
+        *reinterpret_cast<uint4*>(&rows_lds[buf][srow * PITCH + 16 * (spiece + i)]) =
+            live ? held[i] : uint4{0, 0, 0, 0};
+      if (spiece == 0)
+        meta[buf][srow] = Meta{live ? mine.lse * kLog2e : 0.0f, live ? mine.weight : 0.0f,
+                               live ? mine.last : -1, mine.pos};
+    };
+
+    f32x4 sum[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int s = useful(part * per), buf = 0;
+    if (s < stage1) {
+      fetch(s);
+      store(0);
+    }
+    __syncthreads();
+    while (s < stage1) {
+      const int next = useful(s + 1);
+      if (next < stage1) fetch(next);
+#pragma unroll
+      for (int h = 0; h < kStageRows / 16; ++h) {
+        const Meta me = meta[buf][16 * h + m];
+        // nothing to add where no row of the tile sees a token of the wave
+        if (__ballot(me.last >= tok) == 0) continue;
+        const bool masked = DRAFT || __ballot(me.last < tok + 16 * NT) != 0;
+        uint4 qf[NP];
+#pragma unroll
+        for (int a = 0; a < NP; ++a)
+          qf[a] = *reinterpret_cast<const uint4*>(&rows_lds[buf][(16 * h + m) * PITCH + 64 * a + 16 * qg]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const f32x4 z = logits<T, D>(kf[t], qf);
+          if (masked) {
+            uint32_t bits = 0;
+            if constexpr (DRAFT) {
+              const int j0 = tok + 16 * t;
+              if (me.last >= 0 && j0 < n) {
+                if (at.tree)
+                  bits = at.tree[((int64_t)un.b * w + me.pos) * at.tree_words + (j0 >> 5)] >> (j0 & 31);
+                else
+                  bits = me.pos < j0 ? 0u : me.pos - j0 >= 31 ? ~0u : (2u << (me.pos - j0)) - 1u;
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool see = DRAFT ? (bits >> (4 * qg + e) & 1) : tok + 16 * t + 4 * qg + e <= me.last;
+              const float y = exp2_fast(__builtin_fmaf(z[e], at.c, -me.lse));
+              sum[t][e] = see ? __builtin_fmaf(y, me.weight, sum[t][e]) : sum[t][e];
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sum[t][e] = __builtin_fmaf(exp2_fast(__builtin_fmaf(z[e], at.c, -me.lse)), me.weight, sum[t][e]);
+          }
         }
       }
+      if (next < stage1) store(buf ^ 1);
+      __syncthreads();
+      buf ^= 1;
+      s = next;
+    }
+    // over the tile's 16 rows: every lane of a 16-lane group ends with the sums
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float mine = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float pw = exp2_fast(__builtin_fmaf(z[e], at.c, -ls));
-        if (masked) {
-          const bool see = DRAFT ? (bits >> (4 * qg + e) & 1) : tok + 16 * t + 4 * qg + e <= last;
-          pw = see ? pw : 0.0f;
-        }
-        sum[t][e] = masked && !live ? sum[t][e] : __builtin_fmaf(pw, rw, sum[t][e]);
+        float s = sum[t][e];
+        s += dpp_f32<kDppQuadXor1>(s);
+        s += dpp_f32<kDppQuadXor2>(s);
+        s += dpp_f32<kDppHalfMirror>(s);
+        s += dpp_f32<kDppMirror>(s);
+        mine = m == e ? s : mine;
       }
-    }
-  }
-  // over the tile's 16 rows: every lane of a 16-lane group ends with the sums
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    float mine = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float s = sum[t][e];
-      s += dpp_f32<kDppQuadXor1>(s);
-      s += dpp_f32<kDppQuadXor2>(s);
-      s += dpp_f32<kDppHalfMirror>(s);
-      s += dpp_f32<kDppMirror>(s);
-      mine = m == e ? s : mine;
-    }
-    const int j = tok + 16 * t + 4 * qg + m;
-    if (m < 4 && j < n) {
-      if constexpr (DRAFT) {
-        p.acc[(int64_t)u * w + j] = mine;
-      } else {
-        const int64_t i = token_row(g, un) + j;
-        if (row_splits > 1) {
-          p.part[(int64_t)part * g.L * g.H * g.T + i] = mine;
+      const int j = tok + 16 * t + 4 * qg + m;
+      if (m < 4 && j < n) {
+        if constexpr (DRAFT) {
+          p.acc[(int64_t)u * w + j] = mine;
         } else {
-          const float old = p.acc[i];
-          if (!(old < 0.0f)) p.acc[i] = at.decay > 0.0f ? __builtin_fmaf(at.decay, old, mine) : mine;
+          const int64_t i = token_row(g, un) + j;
+          if (row_splits > 1) {
+            p.part[(int64_t)part * g.L * g.H * g.T + i] = mine;
+          } else {
+            const float old = p.acc[i];
+            if (!(old < 0.0f)) p.acc[i] = at.decay > 0.0f ? __builtin_fmaf(at.decay, old, mine) : mine;
+          }
         }
       }
     }
   }
+  if (blockIdx.x == 0 && p.status) write_status(g, p.status);
 }
 
 // The row parts' sums, in order.
