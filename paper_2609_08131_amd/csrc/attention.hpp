@@ -129,9 +129,14 @@ __device__ __forceinline__ void write_status(const Geo& g, uint32_t* status) {
   if (threadIdx.x == 0) *status = bad ? (uint32_t)JACAP_FLAG_BAD_OFFSETS : 0u;
 }
 
-// Running maximum m and sum l of a softmax over one lane's or workgroup's part,
-// in powers of two, joined over parts: exp2(m - ref), with ref finite.
-__device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.0f : m; }
+// A softmax's part holds the maximum its weights refer to (in powers of two) and
+// their sum. Before its first logit the maximum is the lowest finite number, so
+// that neither -inf - (-inf) nor a test for it arises: exp2(-inf - ref) and
+// exp2(ref - larger) are 0. It is raised only when a logit exceeds it by more
+// than kLazyMax, so most steps rescale nothing; the weights stay below 2^8, far
+// inside fp32 and bf16.
+constexpr float kNoMax = -3.402823466e+38f;
+constexpr float kLazyMax = 8.0f;
 
 // ---------------------------------------------------------------------------
 // Workspaces (byte offsets; the status word at 0) and launchers

@@ -38,11 +38,6 @@ struct AttendArgs {
   uint32_t* status;
 };
 
-// The maximum a row's weights refer to is raised only when a logit exceeds it
-// by more than this many powers of two, so most steps neither reduce over lanes nor
-// rescale the output; the weights stay below 2^8, far inside fp32 and bf16.
-constexpr float kLazyMax = 8.0f;
-
 // What the accumulators do in a call, apart in the code: a load or store that
 // only some calls make would have the others' waits count it too.
 enum Mode { kPlain, kHides, kKeeps };  // not read; hide empty slots; and the logits are kept
@@ -91,11 +86,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
   }
 
   f32x4 o[MT][W::kBlocks];
-  float mx[MT], thr[MT], ref[MT], l[MT];
+  float ref[MT], l[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    mx[i] = thr[i] = -INFINITY;
-    ref[i] = l[i] = 0.0f;
+    ref[i] = kNoMax;
+    l[i] = 0.0f;
 #pragma unroll
     for (int b = 0; b < W::kBlocks; ++b) o[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -215,26 +210,32 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
         }
       }
     }
+    float top[MT], over = -INFINITY;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      float top = z[i][0][0];
+      top[i] = z[i][0][0];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, z[i][t][e]);
-      top *= at.c;
-      if (__ballot(top > thr[i]) != 0) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = fmaxf(mx[i], top), nref = finite_ref(now);
-        const float f = exp2_fast(mx[i] - nref);
-        mx[i] = now;
-        thr[i] = now + kLazyMax;
-        ref[i] = nref;
+        for (int e = 0; e < 4; ++e) top[i] = fmaxf(top[i], z[i][t][e]);
+      over = fmaxf(over, __builtin_fmaf(top[i], at.c, -ref[i]));
+    }
+    if (__ballot(over > kLazyMax) != 0) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        float now = top[i] * at.c;
+        now = fmaxf(now, __shfl_xor(now, 16));
+        now = fmaxf(now, __shfl_xor(now, 32));
+        now = fmaxf(now, ref[i]);
+        const float f = exp2_fast(ref[i] - now);
+        ref[i] = now;
         l[i] *= f;
 #pragma unroll
         for (int b = 0; b < W::kBlocks; ++b) o[i][b] *= f;
       }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -242,7 +243,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
           z[i][t][e] = exp2_fast(__builtin_fmaf(z[i][t][e], at.c, -ref[i]));
           l[i] += z[i][t][e];
         }
-    }
     if constexpr (W::kBf16) {
       bf8 pb[MT];
 #pragma unroll
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     l[i] += __shfl_xor(l[i], 16);
     l[i] += __shfl_xor(l[i], 32);
     if (qg == 0) {
-      sm[wave][16 * i + m] = mx[i];
+      sm[wave][16 * i + m] = ref[i];
       sl[wave][16 * i + m] = l[i];
     }
   }
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
   for (int i = 0; i < MT; ++i) {
     float top = sm[0][16 * i + m];
     for (int x = 1; x < 4; ++x) top = fmaxf(top, sm[x][16 * i + m]);
-    const float f = exp2_fast(mx[i] - finite_ref(top));
+    const float f = exp2_fast(ref[i] - top);
     if (i > 0) __syncthreads();
 #pragma unroll
     for (int b = 0; b < NL; ++b)
@@ -394,13 +394,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     const int r = (rb * MT + i) * 16 + jr;
     float jt = sm[0][16 * i + jr];
     for (int x = 1; x < 4; ++x) jt = fmaxf(jt, sm[x][16 * i + jr]);
-    const float jref = finite_ref(jt);
     float sum = 0.0f, val[PER];
 #pragma unroll
     for (int c = 0; c < PER; ++c) val[c] = 0.0f;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      sum += sl[x][16 * i + jr] * exp2_fast(sm[x][16 * i + jr] - jref);
+      sum += sl[x][16 * i + jr] * exp2_fast(sm[x][16 * i + jr] - jt);
 #pragma unroll
       for (int c = 0; c < PER; ++c) val[c] += red[x][jr][jc + c];
     }
@@ -490,10 +489,9 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     const int64_t ur = (int64_t)u * R + r;
     const float2* ml = p.ml + ur * splits;
     __shared__ float red[4];
-    float top = -INFINITY;
+    float top = kNoMax;
     for (int s = tid; s < nsp; s += kThreads) top = fmaxf(top, ml[s].x);
     top = block_combine(wave_max(top), red, [](float a, float b) { return fmaxf(a, b); });
-    const float ref = finite_ref(top);
     // thread: 4 channels of every NG-th chunk
     constexpr int NG = kThreads / (D / 4);
     const int c = tid % (D / 4) * 4, grp = tid / (D / 4);
@@ -502,7 +500,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     float l = 0.0f;
 #pragma unroll 4
     for (int s = grp; s < nsp; s += NG) {
-      const float f = exp2_fast(ml[s].x - ref);
+      const float f = exp2_fast(ml[s].x - top);
       l += ml[s].y * f;
       sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * D) * f;
     }
@@ -553,19 +551,19 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   {
     // 16 threads per row
     const int r = tid >> 4;
-    float top = -INFINITY, l = 0.0f;
+    float top = kNoMax, l = 0.0f;
     const float2* ml = p.ml + ((int64_t)u * R + min(r, R - 1)) * splits;
     for (int s = tid & 15; s < nsp; s += 16) {
       const float2 c = ml[s];
-      const float now = fmaxf(top, c.x), ref = finite_ref(now);
-      l = l * exp2_fast(top - ref) + c.y * exp2_fast(c.x - ref);
+      const float now = fmaxf(top, c.x);
+      l = l * exp2_fast(top - now) + c.y * exp2_fast(c.x - now);
       top = now;
     }
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) {
       const float t = __shfl_xor(top, x), m = __shfl_xor(l, x);
-      const float now = fmaxf(top, t), ref = finite_ref(now);
-      l = l * exp2_fast(top - ref) + m * exp2_fast(t - ref);
+      const float now = fmaxf(top, t);
+      l = l * exp2_fast(top - now) + m * exp2_fast(t - now);
       top = now;
     }
     if ((tid & 15) == 0) {

@@ -14,6 +14,23 @@
 
 namespace jacap {
 
+// Asks for the vector operations of one 16-row tile's logits, then in turn for one MFMA
+// and the operations of one logit (an FMA, an exponential, an addition) over the rest of the
+// block it stands in: the MFMAs run while the others are issued, and a chain's
+// next MFMA finds its predecessor done. fp32 products take longer than the exponentials
+// anyway.
+template <bool BF16, int MFMAS>
+__device__ __forceinline__ void interleave() {
+  if constexpr (BF16) {
+    __builtin_amdgcn_sched_group_barrier(0x002, 12, 0);
+#pragma unroll
+    for (int i = 0; i < MFMAS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // lse: a workgroup takes 16 MT rows of a unit and a chunk of its tokens; the
 // waves take the chunk's 16-token steps in turn, each lane with a maximum and
@@ -27,20 +44,17 @@ struct LseArgs {
   float2* ml;        // else [U][R][chunks]
 };
 
-constexpr float kLazyLse = 8.0f;  // as the attention's: a lane's maximum is raised past this
-
 template <typename T, int D, int MT>
-__global__ __launch_bounds__(kThreads) void attn_lse_kernel(Geo g, Attn at, LseArgs<T> p, int chunk,
+__global__ __launch_bounds__(kThreads, 2) void attn_lse_kernel(Geo g, Attn at, LseArgs<T> p, int chunk,
                                                             int chunks, int row_blocks) {
   using W = Row<T, D>;
   constexpr int NP = W::kPieces;
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int x = blockIdx.x;
-  const int split = x % chunks;
-  x /= chunks;
-  // the last rows of a causal prompt see the most: first
-  const int rb = row_blocks - 1 - x % row_blocks, u = x / row_blocks;
+  // The last rows of a causal prompt see the most: they go first, in every unit.
+  // Units innermost: the workgroups of one unit then share few XCDs and their L2.
+  const int u = blockIdx.x % g.U, x = blockIdx.x / g.U;
+  const int split = x % chunks, rb = row_blocks - 1 - x / chunks;
   const Unit un = live_unit(g, u);
   const int R = at.R, w = g.w;
   const int first = un.n - w;  // position of row 0 (causal)
@@ -55,11 +69,11 @@ __global__ __launch_bounds__(kThreads) void attn_lse_kernel(Geo g, Attn at, LseA
   const int all = at.causal ? first + pmin + 1 : un.n;  // every row sees the tokens below
   const int t0 = split * chunk, t1 = min(limit, t0 + chunk);
 
-  float mx[MT], thr[MT], ref[MT], l[MT];
+  float ref[MT], l[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    mx[i] = thr[i] = -INFINITY;
-    ref[i] = l[i] = 0.0f;
+    ref[i] = kNoMax;
+    l[i] = 0.0f;
   }
   if (t0 < t1) {
     uint4 qf[MT][NP];
@@ -73,53 +87,71 @@ __global__ __launch_bounds__(kThreads) void attn_lse_kernel(Geo g, Attn at, LseA
     const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
     const int32_t ks = (int32_t)(g.kst * sizeof(T));
     const auto acc_range = buffer_range(p.acc + token_row(g, un) + t0, 4 * (t1 - t0));
-    uint4 kf[NP];
-    float a;
+    // The loop holds a step's logits, and forms the next step's tile by tile in their
+    // place as they are added: no branch between, so that a tile's products run beside
+    // the exponentials of the next. Keys are requested a step ahead of their products.
+    struct Keys {
+      uint4 k[NP];
+      float a;
+    };
     // (zeros past the chunk's end)
-    auto load = [&](int r0) {
+    auto load = [&](Keys& x, int r0) {
       const auto kr = buffer_range(kb + r0 * g.kst, rows_bytes(min(16, t1 - r0), ks, W::kBytes));
 #pragma unroll
-      for (int x = 0; x < NP; ++x) kf[x] = buffer_load16(kr, m * ks + 64 * x + 16 * qg);
-      a = buffer_load_f32(acc_range, 4 * (r0 - t0 + m));
+      for (int y = 0; y < NP; ++y) x.k[y] = buffer_load16(kr, m * ks + 64 * y + 16 * qg);
+      x.a = buffer_load_f32(acc_range, 4 * (r0 - t0 + m));
     };
-    load(t0 + 16 * wave);
-    for (int r0 = t0 + 16 * wave; r0 < t1; r0 += 64) {
-      // the next step's keys are requested before this one is multiplied
-      uint4 kc[NP];
+    int r0 = t0 + 16 * wave;
+    Keys cur, next;
+    load(cur, r0);
+    f32x4 z[MT];
 #pragma unroll
-      for (int x = 0; x < NP; ++x) kc[x] = kf[x];
-      const int rows = min(16, t1 - r0);
-      const uint32_t vis = ((1u << rows) - 1) & ~(uint32_t)__ballot(a < 0.0f);
-      load(r0 + 64);
-      const bool masked = r0 + 16 > all || (vis & 0xFFFF) != 0xFFFF;
-      const uint32_t seen = vis >> (4 * qg);
+    for (int i = 0; i < MT; ++i) z[i] = logits<T, D>(cur.k, qf[i]);
+    float sign = cur.a;  // of the step the logits are of
+    load(next, r0 + 64);
+    for (; r0 < t1; r0 += 64) {
+      const uint32_t vis = ((1u << min(16, t1 - r0)) - 1) & ~(uint32_t)__ballot(sign < 0.0f);
+      cur = next;
+      sign = cur.a;
+      load(next, r0 + 128);
+      if (vis != 0xFFFFu || r0 + 16 > all) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = 4 * qg + e;
+            z[i][e] = (vis >> j & 1) && r0 + j <= last[i] ? z[i][e] : -INFINITY;
+          }
+      }
+      float top[MT], over = -INFINITY;
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        f32x4 z = logits<T, D>(kc, qf[i]);
-        if (masked) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            z[e] = (seen >> e & 1) && r0 + 4 * qg + e <= last[i] ? z[e] : -INFINITY;
-        }
-        const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) * at.c;
-        if (top > thr[i]) {
-          const float nref = finite_ref(top);
-          l[i] *= exp2_fast(mx[i] - nref);
-          mx[i] = top;
-          thr[i] = top + kLazyLse;
-          ref[i] = nref;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) l[i] += exp2_fast(__builtin_fmaf(z[e], at.c, -ref[i]));
+        top[i] = fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3]));
+        over = fmaxf(over, __builtin_fmaf(top[i], at.c, -ref[i]));
       }
+      if (__ballot(over > kLazyMax) != 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const float now = fmaxf(ref[i], top[i] * at.c);
+          l[i] *= exp2_fast(ref[i] - now);
+          ref[i] = now;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l[i] += exp2_fast(__builtin_fmaf(z[i][e], at.c, -ref[i]));
+        z[i] = logits<T, D>(cur.k, qf[i]);
+      }
+interleave<W::kBf16, MT * NP>();
     }
   }
   __shared__ float sm[4][16 * MT], sl[4][16 * MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    float top = fmaxf(mx[i], __shfl_xor(mx[i], 16));
+    float top = fmaxf(ref[i], __shfl_xor(ref[i], 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    float s = l[i] * exp2_fast(mx[i] - finite_ref(top));
+    float s = l[i] * exp2_fast(ref[i] - top);
     s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
     if (qg == 0) {
@@ -131,9 +163,8 @@ __global__ __launch_bounds__(kThreads) void attn_lse_kernel(Geo g, Attn at, LseA
   if (tid < 16 * MT && rr0 + tid < R) {
     float top = sm[0][tid];
     for (int y = 1; y < 4; ++y) top = fmaxf(top, sm[y][tid]);
-    const float rf = finite_ref(top);
     float s = 0.0f;
-    for (int y = 0; y < 4; ++y) s += sl[y][tid] * exp2_fast(sm[y][tid] - rf);
+    for (int y = 0; y < 4; ++y) s += sl[y][tid] * exp2_fast(sm[y][tid] - top);
     const int r = rr0 + tid;
     if (chunks > 1) {
       p.ml[((int64_t)u * R + r) * chunks + split] = float2{top, s};
@@ -150,13 +181,12 @@ __global__ __launch_bounds__(kThreads) void attn_lse_join_kernel(Geo g, Attn at,
                                                                  float* lse, int chunks) {
   const int64_t ur = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
   const bool live = ur < (int64_t)g.U * at.R;
-  float top = -INFINITY, l = 0.0f;
+  float top = kNoMax, l = 0.0f;
   const float2* src = ml + (live ? ur : 0) * chunks;
   for (int s = threadIdx.x & 15; s < chunks; s += 16) top = fmaxf(top, src[s].x);
 #pragma unroll
   for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-  const float ref = finite_ref(top);
-  for (int s = threadIdx.x & 15; s < chunks; s += 16) l += src[s].y * exp2_fast(src[s].x - ref);
+  for (int s = threadIdx.x & 15; s < chunks; s += 16) l += src[s].y * exp2_fast(src[s].x - top);
 #pragma unroll
   for (int x = 8; x > 0; x >>= 1) l += __shfl_xor(l, x);
   if (live && (threadIdx.x & 15) == 0)
@@ -192,13 +222,10 @@ hipError_t launch_attn_lse(const AttnLaunch& A, const WeightsSpace& w, const voi
 
 // ---------------------------------------------------------------------------
 // Sums: a workgroup takes 64 NT tokens of a unit, 16 NT per wave with their keys in
-// registers, and a part of the rows, kStageRows at a time through LDS (two
+// registers, and a part of the rows, a stage of them at a time through LDS (two
 // buffers, the next rows requested a stage ahead). A lane adds the weights its
 // query row gives its tokens; the 16 lanes of a tile's rows are added at the
 // end. DRAFT: the tokens are the drafted ones, seen by the tree's mask.
-//
-// A staged row has 16 bytes of padding: the 16 lanes that read one piece of 16
-// rows then touch all banks.
 // ---------------------------------------------------------------------------
 template <typename T>
 struct SumArgs {
@@ -209,25 +236,20 @@ struct SumArgs {
   uint32_t* status;   // or null
 };
 
-constexpr int kStageRows = 32;
-
 template <typename T, int D, int NT, bool DRAFT>
 __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumArgs<T> p, int blocks,
                                                             int row_splits) {
   using W = Row<T, D>;
   constexpr int NP = W::kPieces;
-  constexpr int PITCH = W::kBytes + 16;
-  constexpr int SHARE = kStageRows * W::kBytes / 16 / kThreads;  // 16-byte pieces per thread and stage
-  constexpr int LANES = W::kBytes / 16 / SHARE;                  // threads per staged row
-  static_assert(LANES * kStageRows == kThreads, "a thread stages one row's pieces");
+  constexpr int TILES = W::kBf16 ? 4 : 2;        // 16-row tiles per stage
+  constexpr int ROWS = 16 * TILES;
+  constexpr int PW = TILES * NP / 4;             // pieces per thread and stage, of one row
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // row parts of a token block together; a causal prompt's first tokens, which
-  // the most rows see, first
-  int x = blockIdx.x;
-  const int part = x % row_splits;
-  x /= row_splits;
-  const int u = x % g.U, blk = x / g.U;
+  // units innermost, as above; a causal prompt's first tokens, which the most rows
+  // see, first
+  const int u = blockIdx.x % g.U, x = blockIdx.x / g.U;
+  const int part = x % row_splits, blk = x / row_splits;
   const Unit un = live_unit(g, u);
   const int n = DRAFT ? g.w : un.n;
   const int btok = blk * 64 * NT;            // the workgroup's first token
@@ -235,19 +257,9 @@ __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumA
   const int R = at.R, w = g.w;
   const bool causal = !DRAFT && at.causal;
   const int first = causal ? un.n - w : 0;
-  const int stages = (R + kStageRows - 1) / kStageRows;
+  const int stages = (R + ROWS - 1) / ROWS;
   const int per = (stages + row_splits - 1) / row_splits;
   const int stage1 = min(stages, (part + 1) * per);
-  // The first stage from s on with a row that sees the workgroup's tokens: whole
-  // stages of one head whose positions all lie before them are skipped.
-  auto useful = [&](int s) {
-    if (causal && s < stage1) {
-      const int r0 = s * kStageRows, head = r0 / w, p0 = r0 - head * w;
-      if (p0 + kStageRows <= w && first + p0 + kStageRows - 1 < btok)
-        s = (head * w + min(w, btok - first)) / kStageRows;
-    }
-    return s;
-  };
 
   if (btok < n) {
     const int64_t kst = DRAFT ? at.dkr : g.kst;
@@ -266,88 +278,160 @@ __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumA
     const float* lseu = p.lse + ((int64_t)un.b * g.L + un.l) * g.Hq * w + (int64_t)un.h * R;
     const float* rwu = at.row_weight ? at.row_weight + (int64_t)un.b * w : nullptr;
 
-    __shared__ __align__(16) char rows_lds[2][kStageRows * PITCH];
+    // Staged rows lie as the MFMA takes them: piece a of tile h, 16 bytes per lane.
+    __shared__ __align__(16) uint4 rows_lds[2][TILES][NP][64];
     struct Meta { float lse, weight; int last, pos; };  // last position seen, -1: adds nothing
-    __shared__ Meta meta[2][kStageRows];
-    const int srow = tid / LANES, spiece = tid % LANES * SHARE;
-    uint4 held[SHARE];
+    __shared__ Meta meta[2][ROWS];
+    // The row a thread stages: row m of tile `stile`, pieces sa .. sa + PW - 1. Its head
+    // and position are carried from stage to stage (a division each would cost more
+    // than a row's logits).
+    const int stile = wave * PW / NP, sa = wave * PW % NP;
+    int stage = 0, row = 0, pos = 0, head = 0;
+    int p0 = 0, h0 = 0;  // of the stage's first row
+    auto seek = [&](int to) {
+      stage = to;
+      h0 = to * ROWS / w;
+      p0 = to * ROWS - h0 * w;
+      row = to * ROWS + stile * 16 + m;
+      head = row / w;
+      pos = row - head * w;
+    };
+    // The next stage with a row that sees the workgroup's tokens: stages of one
+    // head whose positions all lie before them are skipped.
+    auto skip = [&] {
+      while (causal && stage < stage1 && p0 + ROWS <= w && first + p0 + ROWS - 1 < btok)
+        seek((h0 * w + min(w, btok - first)) / ROWS);
+    };
+    auto advance = [&] {
+      ++stage;
+      p0 += ROWS;
+      while (p0 >= w) {
+        p0 -= w;
+        ++h0;
+      }
+      row += ROWS;
+      pos += ROWS;
+      while (pos >= w) {
+        pos -= w;
+        ++head;
+      }
+      skip();
+    };
+    uint4 held[PW];
     Meta mine;
-    auto fetch = [&](int s) {
-      const int r = min(s * kStageRows + srow, R - 1);
-      const int head = r / w, pos = r - head * w;
-      const char* src = reinterpret_cast<const char*>(qu + head * g.qsh + pos * g.qsp);
+    auto fetch = [&] {
+      // (rows past the last are its copies, and add nothing)
+      const int hh = row < R ? head : g.G - 1, pp = row < R ? pos : w - 1;
+      const char* src = reinterpret_cast<const char*>(qu + hh * g.qsh + pp * g.qsp) + 64 * sa + 16 * qg;
 #pragma unroll
-      for (int i = 0; i < SHARE; ++i) held[i] = *reinterpret_cast<const uint4*>(src + 16 * (spiece + i));
-      mine.lse = lseu[r];
-      mine.weight = rwu ? rwu[pos] : 1.0f;
-      mine.pos = pos;
-      mine.last = s * kStageRows + srow < R ? (causal ? first + pos : INT32_MAX) : -1;
+      for (int i = 0; i < PW; ++i) held[i] = *reinterpret_cast<const uint4*>(src + 64 * i);
+      mine.lse = lseu[min(row, R - 1)];
+      mine.weight = rwu ? rwu[pp] : 1.0f;
+      mine.pos = pp;
+      mine.last = row < R ? (causal ? first + pp : INT32_MAX) : -1;
     };
     auto store = [&](int buf) {
       const bool live = mine.last >= 0 && mine.weight != 0.0f && mine.lse != -INFINITY;
 #pragma unroll
-      for (int i = 0; i < SHARE; ++i)
-        *reinterpret_cast<uint4*>(&rows_lds[buf][srow * PITCH + 16 * (spiece + i)]) =
-            live ? held[i] : uint4{0, 0, 0, 0};
-      if (spiece == 0)
-        meta[buf][srow] = Meta{live ? mine.lse * kLog2e : 0.0f, live ? mine.weight : 0.0f,
-                               live ? mine.last : -1, mine.pos};
+      for (int i = 0; i < PW; ++i)
+        rows_lds[buf][stile][sa + i][lane] = live ? held[i] : uint4{0, 0, 0, 0};
+      if (sa == 0 && qg == 0)
+        meta[buf][stile * 16 + m] = Meta{live ? mine.lse * kLog2e : 0.0f, live ? mine.weight : 0.0f,
+                                         live ? mine.last : -1, mine.pos};
     };
 
-    f32x4 sum[NT];
+    // z: the logits of the last row tile, not added yet; its rows' lse and weight
+    f32x4 sum[NT], z[NT];
+    float ls = 0.0f, weight = 0.0f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int s = useful(part * per), buf = 0;
-    if (s < stage1) {
-      fetch(s);
+    for (int t = 0; t < NT; ++t) {
+      sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      z[t] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    }
+    auto add = [&](int t) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sum[t][e] = __builtin_fmaf(exp2_fast(__builtin_fmaf(z[t][e], at.c, -ls)), weight, sum[t][e]);
+    };
+    int buf = 0;
+    seek(part * per);
+    skip();
+    bool more = stage < stage1;
+    if (more) {
+      fetch();
       store(0);
     }
     __syncthreads();
-    while (s < stage1) {
-      const int next = useful(s + 1);
-      if (next < stage1) fetch(next);
+    while (more) {
+      advance();
+      more = stage < stage1;
+      if (more) fetch();
+      Meta me[TILES];
+      bool masked = DRAFT;
 #pragma unroll
-      for (int h = 0; h < kStageRows / 16; ++h) {
-        const Meta me = meta[buf][16 * h + m];
-        // nothing to add where no row of the tile sees a token of the wave
-        if (__ballot(me.last >= tok) == 0) continue;
-        const bool masked = DRAFT || __ballot(me.last < tok + 16 * NT) != 0;
-        uint4 qf[NP];
+      for (int h = 0; h < TILES; ++h) {
+        me[h] = meta[buf][16 * h + m];
+        masked = masked || __ballot(me[h].last < tok + 16 * NT) != 0;
+      }
+      auto row_tile = [&](int h, uint4 (&qf)[NP]) {
 #pragma unroll
         for (int a = 0; a < NP; ++a)
-          qf[a] = *reinterpret_cast<const uint4*>(&rows_lds[buf][(16 * h + m) * PITCH + 64 * a + 16 * qg]);
+          qf[a] = rows_lds[buf][h][a][lane];
+      };
+      if (!masked) {
+        // Every row sees every token: no branch in here. z holds the tile before; each
+        // of its logits is added and the new tile's formed in its place, so that the
+        // exponentials run beside the products, across the stages' ends too.
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const f32x4 z = logits<T, D>(kf[t], qf);
-          if (masked) {
+        for (int h = 0; h < TILES; ++h) {
+          uint4 qf[NP];
+          row_tile(h, qf);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            add(t);
+            z[t] = logits<T, D>(kf[t], qf);
+          }
+          ls = me[h].lse;
+          weight = me[h].weight;
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < TILES; ++h) {
+          // nothing to add where no row of the tile sees a token of the wave
+          if (__ballot(me[h].last >= tok) == 0) continue;
+          uint4 qf[NP];
+          row_tile(h, qf);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            add(t);
+            z[t] = logits<T, D>(kf[t], qf);
             uint32_t bits = 0;
             if constexpr (DRAFT) {
               const int j0 = tok + 16 * t;
-              if (me.last >= 0 && j0 < n) {
+              if (me[h].last >= 0 && j0 < n) {
                 if (at.tree)
-                  bits = at.tree[((int64_t)un.b * w + me.pos) * at.tree_words + (j0 >> 5)] >> (j0 & 31);
+                  bits = at.tree[((int64_t)un.b * w + me[h].pos) * at.tree_words + (j0 >> 5)] >> (j0 & 31);
                 else
-                  bits = me.pos < j0 ? 0u : me.pos - j0 >= 31 ? ~0u : (2u << (me.pos - j0)) - 1u;
+                  bits = me[h].pos < j0 ? 0u : me[h].pos - j0 >= 31 ? ~0u : (2u << (me[h].pos - j0)) - 1u;
               }
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const bool see = DRAFT ? (bits >> (4 * qg + e) & 1) : tok + 16 * t + 4 * qg + e <= me.last;
-              const float y = exp2_fast(__builtin_fmaf(z[e], at.c, -me.lse));
-              sum[t][e] = see ? __builtin_fmaf(y, me.weight, sum[t][e]) : sum[t][e];
+              const bool see =
+                  DRAFT ? (bits >> (4 * qg + e) & 1) : tok + 16 * t + 4 * qg + e <= me[h].last;
+              z[t][e] = see ? z[t][e] : -INFINITY;
             }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              sum[t][e] = __builtin_fmaf(exp2_fast(__builtin_fmaf(z[e], at.c, -me.lse)), me.weight, sum[t][e]);
           }
+          ls = me[h].lse;
+          weight = me[h].weight;
         }
       }
-      if (next < stage1) store(buf ^ 1);
+      if (more) store(buf ^ 1);
       __syncthreads();
       buf ^= 1;
-      s = next;
     }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) add(t);
     // over the tile's 16 rows: every lane of a 16-lane group ends with the sums
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
