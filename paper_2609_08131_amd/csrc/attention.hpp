@@ -26,10 +26,11 @@ constexpr int kAttendChunk = 8192;    // tokens per workgroup of the attention: 
 constexpr int kAttendChunkMin = 256;  // ... and at least
 constexpr int kAttendBlocks = 512;   // chunks shrink until the grid has this many workgroups
 constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
-// The log-sum pass: 16-row tiles per workgroup (their queries in registers),
-// tokens per workgroup.
-constexpr int kLseTilesBf16 = 8, kLseTilesFp32 = 2;
-constexpr int kLseChunk = 8192, kLseChunkMin = 256;
+// The passes with rows in registers: 16-row tiles per workgroup, at most, and tokens.
+constexpr int kRowTilesBf16 = 8, kRowTilesFp32 = 2;
+constexpr int kRowsChunk = 8192, kRowsChunkMin = 256;
+// 16-row tiles per KV head up to which the sums stream the keys past the rows too.
+constexpr int kStreamTilesBf16 = 4, kStreamTilesFp32 = 2;
 // The accumulation: 16-token tiles per wave (their keys in registers); the rows are
 // cut into parts of at least kSumRowsMin while the grid is small.
 constexpr int kSumTilesBf16 = 4, kSumTilesFp32 = 2;
@@ -67,6 +68,14 @@ struct Row {
   static constexpr int kVWords = kVBytes / 4;
   static constexpr int kBlocks = kVLoads * kVec;         // 16-channel blocks of the output
 };
+
+// The larger of three, as the instruction takes them: fmaxf would first quiet each
+// operand that comes out of an MFMA, one instruction each.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -155,10 +164,11 @@ struct AttendSpace {
 };
 
 struct WeightsSpace {
-  int chunk, chunks, mt, row_blocks;  // the log-sum pass: tokens per workgroup, and rows
-  int tiles;           // the accumulation: 16-token tiles per wave
+  int chunk, chunks, mt, row_blocks;  // the passes with rows in registers
+  bool stream_keys;    // the sums are one of them; else with keys in registers:
+  int tiles;           // ... 16-token tiles per wave
   int blocks;          // ... token blocks of the longest sequence
-  int row_splits;      // ... parts the rows are cut into
+  int row_splits;      // parts the rows of the sums are cut into
   size_t ml;           // float2 [U][R][chunks]
   size_t lse;          // float [U][R]
   size_t part;         // float [row_splits][L][H][T]

@@ -85,38 +85,47 @@ int chunk_tokens(const Geo& g, int64_t per, int most, int least, int blocks) {
   return chunk;
 }
 
-// How the accumulation is cut (attn_sum_kernel). With no rows the sums of one
-// part; `o` the workspace's size so far.
+// How the passes over rows and tokens of the weights are cut; `o` the
+// workspace's size so far. The sums of few rows stream the keys past the rows,
+// as the log-sums do; those of more hold keys and stream rows (log-sums and sums of 4
+// rows, 131072 tokens, 8 heads: 89 us streaming keys, 121 holding them; of 128 rows,
+// 8192 tokens: 27 and 26; of 256 rows, 4 layers of 131072: 970 and 875).
 void layout_sum(const Geo& g, const Attn& at, bool bf16, WeightsSpace* w, size_t* o) {
+  const int64_t LHT = (int64_t)g.L * g.H * g.T;
+  const int tiles = (at.R + 15) / 16;
+  w->mt = !bf16 ? kRowTilesFp32 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : kRowTilesBf16;
+  w->row_blocks = (tiles + w->mt - 1) / w->mt;
+  w->chunk = chunk_tokens(g, w->row_blocks, kRowsChunk, kRowsChunkMin, kWeightsBlocks);
+  w->chunks = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
   w->tiles = bf16 ? kSumTilesBf16 : kSumTilesFp32;
   const int tokens = 64 * w->tiles;
   w->blocks = (g.maxn + tokens - 1) / tokens;
-  const int64_t LHT = (int64_t)g.L * g.H * g.T;
+  w->stream_keys = tiles <= (bf16 ? kStreamTilesBf16 : kStreamTilesFp32);
   const int64_t grid = std::max<int64_t>(1, LHT / tokens);
-  w->row_splits = (int)std::max<int64_t>(
-      1, std::min<int64_t>(kWeightsBlocks / grid, at.R / kSumRowsMin));
+  w->row_splits = w->stream_keys
+                      ? 1
+                      : (int)std::max<int64_t>(1, std::min<int64_t>(kWeightsBlocks / grid,
+                                                                    at.R / kSumRowsMin));
   w->part = *o;
   if (w->row_splits > 1) *o = align256(*o + 4 * (size_t)w->row_splits * LHT);
+}
+
+bool sum_grid_ok(const Geo& g, const WeightsSpace& w) {
+  return (int64_t)g.U * w.row_blocks * w.chunks <= kMaxGrid &&
+         (int64_t)g.U * std::max(1, w.blocks) * w.row_splits <= kMaxGrid;
 }
 
 jacap_status layout_weights(const AttnLaunch& A, bool bf16, WeightsSpace* w) {
   const Geo& g = A.base.geo;
   const int64_t UR = (int64_t)g.U * A.at.R;
   size_t o = 256;
-  w->mt = bf16 ? kLseTilesBf16 : kLseTilesFp32;
-  w->row_blocks = (A.at.R + 16 * w->mt - 1) / (16 * w->mt);
-  w->chunk = chunk_tokens(g, w->row_blocks, kLseChunk, kLseChunkMin, kWeightsBlocks);
-  w->chunks = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
+  layout_sum(g, A.at, bf16, w, &o);
   w->lse = o;
   o = align256(o + 4 * (size_t)UR);
   w->ml = o;
   if (w->chunks > 1) o = align256(o + 8 * (size_t)UR * w->chunks);
-  layout_sum(g, A.at, bf16, w, &o);
   w->total = o;
-  if ((int64_t)g.U * w->row_blocks * w->chunks > kMaxGrid || UR / 16 > kMaxGrid ||
-      (int64_t)g.U * std::max(1, w->blocks) * w->row_splits > kMaxGrid)
-    return JACAP_ERR_UNSUPPORTED;
-  return JACAP_OK;
+  return UR / 16 > kMaxGrid || !sum_grid_ok(g, *w) ? JACAP_ERR_UNSUPPORTED : JACAP_OK;
 }
 
 // sum: the accumulation's own cut, for accumulating from more rows than keep
@@ -146,7 +155,7 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   const int64_t pairs = (int64_t)g.U * w->splits + 8;
   const int64_t token_blocks = g.maxn / kJoinTokens + 1;
   if (pairs * w->row_blocks > kMaxGrid || UR + g.U * token_blocks > kMaxGrid ||
-      (int64_t)g.U * std::max(1, sum->blocks) * std::max(1, sum->row_splits) > kMaxGrid)
+      !sum_grid_ok(g, *sum))
     return JACAP_ERR_UNSUPPORTED;
   return JACAP_OK;
 }

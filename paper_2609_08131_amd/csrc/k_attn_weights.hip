@@ -31,22 +31,56 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
+// The sum over a tile's 16 query rows of each of its tokens: lane (m, q) receives
+// that of token 4 q + m for m < 4.
+__device__ __forceinline__ float tile_sum(const f32x4& x, int m) {
+  float mine = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float s = x[e];
+    s += dpp_f32<kDppQuadXor1>(s);
+    s += dpp_f32<kDppQuadXor2>(s);
+    s += dpp_f32<kDppHalfMirror>(s);
+    s += dpp_f32<kDppMirror>(s);
+    mine = m == e ? s : mine;
+  }
+  return mine;
+}
+
+// An accumulator's new value.
+__device__ __forceinline__ float decayed(const Attn& at, float old, float sum) {
+  return at.decay > 0.0f ? __builtin_fmaf(at.decay, old, sum) : sum;
+}
+
 // ---------------------------------------------------------------------------
-// lse: a workgroup takes 16 MT rows of a unit and a chunk of its tokens; the
-// waves take the chunk's 16-token steps in turn, each lane with a maximum and
-// sum of its own (its row's tokens 4 q .. 4 q + 3), joined at the end.
+// Rows in registers, keys streamed. A workgroup takes 16 MT rows of a unit and a
+// chunk of its tokens; the waves take the chunk's 16-token steps in turn.
+//
+// SUM = false, the rows' lse: each lane keeps a maximum and sum of its own (its
+// row's tokens 4 q .. 4 q + 3), joined at the end.
+// SUM = true, the tokens' weights from the rows' known lse, for rows of one block
+// (the other way round a workgroup would load its keys for a handful of row
+// tiles). A step's weights are added over the row tiles in each lane, then
+// over the 16 lanes that hold a tile's rows.
+//
+// The loop holds a step's logits, and forms the next step's tile by tile in their
+// place as they are added: no branch between, so that a tile's products run beside
+// the exponentials of the next. Keys are requested a step ahead of their products.
 // ---------------------------------------------------------------------------
 template <typename T>
-struct LseArgs {
+struct RowArgs {
   const T *q, *k;
-  const float* acc;
-  float* lse;        // [B][L][H_q][w], written here with one chunk
-  float2* ml;        // else [U][R][chunks]
+  float* acc;        // empty slots; SUM: updated
+  const float* lse_in;    // SUM: [B][L][H_q][w]
+  float* lse;        // else [B][L][H_q][w], written here with one chunk
+  float2* ml;        // ... or [U][R][chunks]
+  uint32_t* status;  // or null
 };
 
-template <typename T, int D, int MT>
-__global__ __launch_bounds__(kThreads, 2) void attn_lse_kernel(Geo g, Attn at, LseArgs<T> p, int chunk,
-                                                            int chunks, int row_blocks) {
+template <typename T, int D, int MT, bool SUM>
+__global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, RowArgs<T> p,
+                                                                int chunk, int chunks,
+                                                                int row_blocks) {
   using W = Row<T, D>;
   constexpr int NP = W::kPieces;
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
@@ -65,93 +99,136 @@ __global__ __launch_bounds__(kThreads, 2) void attn_lse_kernel(Geo g, Attn at, L
     pmin = rr0 % w;
     pmax = (rr1 - 1) % w;
   }
-  const int limit = at.causal ? min(un.n, first + pmax + 1) : un.n;
+  // (the sums pass every token: those that no row sees decay)
+  const int limit = at.causal && !SUM ? min(un.n, first + pmax + 1) : un.n;
   const int all = at.causal ? first + pmin + 1 : un.n;  // every row sees the tokens below
   const int t0 = split * chunk, t1 = min(limit, t0 + chunk);
 
-  float ref[MT], l[MT];
+  float nref[MT], l[MT];  // minus the lane's maximum, its sum; SUM: minus lse, the row's weight
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    ref[i] = kNoMax;
+    nref[i] = -kNoMax;
     l[i] = 0.0f;
   }
   if (t0 < t1) {
     uint4 qf[MT][NP];
-    int last[MT];  // position of the lane's row of each tile
+    int last[MT];      // position of the lane's row of each tile; SUM: -1 if it adds nothing
+    bool dead = false;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int r = rr0 + 16 * i + m;
-      load_row<T, D>(g, unit_queries(g, un, p.q), min(r, R - 1), r < R, qg, qf[i]);
-      last[i] = at.causal ? first + r % w : INT32_MAX;
+      const int r = rr0 + 16 * i + m, rc = min(r, R - 1);
+      bool used = r < R;
+      if constexpr (SUM) {
+        const int pos = rc % w;
+        const float ls = p.lse_in[((int64_t)un.b * g.L + un.l) * g.Hq * w + (int64_t)un.h * R + rc];
+        const float weight = at.row_weight ? at.row_weight[(int64_t)un.b * w + pos] : 1.0f;
+        used = used && weight != 0.0f && ls != -INFINITY;
+        nref[i] = used ? -ls * kLog2e : 0.0f;
+        l[i] = used ? weight : 0.0f;
+        dead |= !used;
+      }
+      load_row<T, D>(g, unit_queries(g, un, p.q), rc, used, qg, qf[i]);
+      last[i] = SUM && !used ? -1 : at.causal ? first + rc % w : INT32_MAX;
     }
+    const bool some_dead = SUM && __ballot(dead) != 0;
     const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
     const int32_t ks = (int32_t)(g.kst * sizeof(T));
-    const auto acc_range = buffer_range(p.acc + token_row(g, un) + t0, 4 * (t1 - t0));
-    // The loop holds a step's logits, and forms the next step's tile by tile in their
-    // place as they are added: no branch between, so that a tile's products run beside
-    // the exponentials of the next. Keys are requested a step ahead of their products.
+    const int64_t tr = token_row(g, un) + t0;
+    const auto acc_range = buffer_range(p.acc + tr, 4 * (t1 - t0));
     struct Keys {
       uint4 k[NP];
-      float a;
+      float a;  // the accumulator of token m
     };
     // (zeros past the chunk's end)
-    auto load = [&](Keys& x, int r0) {
+    auto load = [&](Keys& y, int r0) {
       const auto kr = buffer_range(kb + r0 * g.kst, rows_bytes(min(16, t1 - r0), ks, W::kBytes));
 #pragma unroll
-      for (int y = 0; y < NP; ++y) x.k[y] = buffer_load16(kr, m * ks + 64 * y + 16 * qg);
-      x.a = buffer_load_f32(acc_range, 4 * (r0 - t0 + m));
+      for (int a = 0; a < NP; ++a) y.k[a] = buffer_load16(kr, m * ks + 64 * a + 16 * qg);
+      y.a = buffer_load_f32(acc_range, 4 * (r0 - t0 + m));
     };
     int r0 = t0 + 16 * wave;
-    Keys cur, next;
-    load(cur, r0);
+    Keys ka, kb2;
+    load(ka, r0);
     f32x4 z[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) z[i] = logits<T, D>(cur.k, qf[i]);
-    float sign = cur.a;  // of the step the logits are of
-    load(next, r0 + 64);
-    for (; r0 < t1; r0 += 64) {
+    for (int i = 0; i < MT; ++i) z[i] = logits<T, D>(ka.k, qf[i]);
+    float sign = ka.a;  // of the step that z is of
+    load(kb2, r0 + 64);
+    // One step: z's logits are added, `next` gives the following step's, and `far`
+    // takes the keys of the one after that.
+    auto step = [&](const Keys& next, Keys& far) {
       const uint32_t vis = ((1u << min(16, t1 - r0)) - 1) & ~(uint32_t)__ballot(sign < 0.0f);
-      cur = next;
-      sign = cur.a;
-      load(next, r0 + 128);
-      if (vis != 0xFFFFu || r0 + 16 > all) {
+      const float old = sign;
+      sign = next.a;
+      load(far, r0 + 128);
+      // SUM leaves hidden tokens out where it writes; rows that add nothing must not
+      // meet a key that is not finite
+      if ((!SUM && vis != 0xFFFFu) || r0 + 16 > all || some_dead) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int j = 4 * qg + e;
-            z[i][e] = (vis >> j & 1) && r0 + j <= last[i] ? z[i][e] : -INFINITY;
+            z[i][e] = (SUM || (vis >> j & 1)) && r0 + j <= last[i] ? z[i][e] : -INFINITY;
           }
       }
-      float top[MT], over = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        top[i] = fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3]));
-        over = fmaxf(over, __builtin_fmaf(top[i], at.c, -ref[i]));
-      }
-      if (__ballot(over > kLazyMax) != 0) {
+      if constexpr (!SUM) {
+        float top[MT], over = kNoMax;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          const float now = fmaxf(ref[i], top[i] * at.c);
-          l[i] *= exp2_fast(ref[i] - now);
-          ref[i] = now;
+          top[i] = max3(max3(z[i][0], z[i][1], z[i][2]), z[i][3], z[i][3]);
+          over = max3(over, __builtin_fmaf(top[i], at.c, nref[i]), over);
+        }
+        if (__ballot(over > kLazyMax) != 0) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            const float now = fmaxf(-nref[i], top[i] * at.c);
+            l[i] *= exp2_fast(-nref[i] - now);
+            nref[i] = -now;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) l[i] += exp2_fast(__builtin_fmaf(z[i][e], at.c, nref[i]));
+          z[i] = logits<T, D>(next.k, qf[i]);
+        }
+        interleave<W::kBf16, MT * NP>();
+      } else {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sum[e] = __builtin_fmaf(exp2_fast(__builtin_fmaf(z[i][e], at.c, nref[i])), l[i], sum[e]);
+          z[i] = logits<T, D>(next.k, qf[i]);
+        }
+        interleave<W::kBf16, MT * NP>();
+        const float mine = tile_sum(sum, m);
+        const int j = 4 * qg + m;  // lanes m < 4 hold token j; its accumulator is lane j's
+        const float oldj = __shfl(old, j & 15);
+        if (m < 4 && r0 + j < t1) {
+          if (!(oldj < 0.0f)) p.acc[tr + (r0 - t0 + j)] = decayed(at, oldj, mine);
         }
       }
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) l[i] += exp2_fast(__builtin_fmaf(z[i][e], at.c, -ref[i]));
-        z[i] = logits<T, D>(cur.k, qf[i]);
-      }
-interleave<W::kBf16, MT * NP>();
+      r0 += 64;
+    };
+    while (r0 < t1) {
+      step(kb2, ka);
+      if (r0 >= t1) break;
+      step(ka, kb2);
     }
+  }
+  if constexpr (SUM) {
+    if (blockIdx.x == 0 && p.status) write_status(g, p.status);
+    return;
   }
   __shared__ float sm[4][16 * MT], sl[4][16 * MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    float top = fmaxf(ref[i], __shfl_xor(ref[i], 16));
+    float top = fmaxf(-nref[i], __shfl_xor(-nref[i], 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    float s = l[i] * exp2_fast(ref[i] - top);
+    float s = l[i] * exp2_fast(-nref[i] - top);
     s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
     if (qg == 0) {
@@ -194,19 +271,36 @@ __global__ __launch_bounds__(kThreads) void attn_lse_join_kernel(Geo g, Attn at,
     lse[ur] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
 }
 
-template <typename T, int D, int MT>
+template <typename T, int D, int MT, bool SUM>
+static hipError_t rows_typed(const AttnLaunch& A, const WeightsSpace& w, const RowArgs<T>& p) {
+  const Geo& g = A.base.geo;
+  attn_rows_kernel<T, D, MT, SUM>
+      <<<(unsigned)((int64_t)g.U * w.row_blocks * w.chunks), kThreads, 0, A.base.stream>>>(
+          g, A.at, p, w.chunk, w.chunks, w.row_blocks);
+  return hipGetLastError();
+}
+
+template <typename T, int D, bool SUM>
+static hipError_t rows_tiles(const AttnLaunch& A, const WeightsSpace& w, const RowArgs<T>& p) {
+  if constexpr (sizeof(T) == 2) {
+    if constexpr (!SUM)
+      if (w.mt == 8) return rows_typed<T, D, 8, SUM>(A, w, p);
+    if (w.mt == 4) return rows_typed<T, D, 4, SUM>(A, w, p);
+  }
+  return rows_typed<T, D, 2, SUM>(A, w, p);
+}
+
+template <typename T, int D>
 static hipError_t lse_typed(const AttnLaunch& A, const WeightsSpace& w, const void* q, const void* k,
                             const float* acc, float* lse) {
   const Geo& g = A.base.geo;
-  LseArgs<T> p{(const T*)q, (const T*)k, acc, lse, ws_ptr<float2>(A.base.wsp, w.ml)};
-  const int64_t grid = (int64_t)g.U * w.row_blocks * w.chunks;
-  attn_lse_kernel<T, D, MT><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, w.chunk,
-                                                                            w.chunks, w.row_blocks);
-  if (w.chunks > 1) {
-    const int64_t rows = (int64_t)g.U * A.at.R;
-    attn_lse_join_kernel<<<(unsigned)((rows + 15) / 16), kThreads, 0, A.base.stream>>>(
-        g, A.at, p.ml, lse, w.chunks);
-  }
+  RowArgs<T> p{(const T*)q, (const T*)k, const_cast<float*>(acc), nullptr, lse,
+               ws_ptr<float2>(A.base.wsp, w.ml), nullptr};
+  const hipError_t e = rows_tiles<T, D, false>(A, w, p);
+  if (e != hipSuccess || w.chunks == 1) return e;
+  const int64_t rows = (int64_t)g.U * A.at.R;
+  attn_lse_join_kernel<<<(unsigned)((rows + 15) / 16), kThreads, 0, A.base.stream>>>(
+      g, A.at, p.ml, lse, w.chunks);
   return hipGetLastError();
 }
 
@@ -214,10 +308,10 @@ hipError_t launch_attn_lse(const AttnLaunch& A, const WeightsSpace& w, const voi
                            const float* acc, float* lse) {
   const bool wide = A.base.geo.D == 128;
   if (A.base.cfg->dtype == JACAP_DTYPE_BF16)
-    return wide ? lse_typed<__bf16, 128, kLseTilesBf16>(A, w, q, k, acc, lse)
-                : lse_typed<__bf16, 64, kLseTilesBf16>(A, w, q, k, acc, lse);
-  return wide ? lse_typed<float, 128, kLseTilesFp32>(A, w, q, k, acc, lse)
-              : lse_typed<float, 64, kLseTilesFp32>(A, w, q, k, acc, lse);
+    return wide ? lse_typed<__bf16, 128>(A, w, q, k, acc, lse)
+                : lse_typed<__bf16, 64>(A, w, q, k, acc, lse);
+  return wide ? lse_typed<float, 128>(A, w, q, k, acc, lse)
+              : lse_typed<float, 64>(A, w, q, k, acc, lse);
 }
 
 // ---------------------------------------------------------------------------
@@ -237,7 +331,7 @@ struct SumArgs {
 };
 
 template <typename T, int D, int NT, bool DRAFT>
-__global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumArgs<T> p, int blocks,
+__global__ __launch_bounds__(kThreads, 2) void attn_sum_kernel(Geo g, Attn at, SumArgs<T> p, int blocks,
                                                             int row_splits) {
   using W = Row<T, D>;
   constexpr int NP = W::kPieces;
@@ -432,19 +526,9 @@ __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumA
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) add(t);
-    // over the tile's 16 rows: every lane of a 16-lane group ends with the sums
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      float mine = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float s = sum[t][e];
-        s += dpp_f32<kDppQuadXor1>(s);
-        s += dpp_f32<kDppQuadXor2>(s);
-        s += dpp_f32<kDppHalfMirror>(s);
-        s += dpp_f32<kDppMirror>(s);
-        mine = m == e ? s : mine;
-      }
+      const float mine = tile_sum(sum[t], m);
       const int j = tok + 16 * t + 4 * qg + m;
       if (m < 4 && j < n) {
         if constexpr (DRAFT) {
@@ -455,7 +539,7 @@ __global__ __launch_bounds__(kThreads) void attn_sum_kernel(Geo g, Attn at, SumA
             p.part[(int64_t)part * g.L * g.H * g.T + i] = mine;
           } else {
             const float old = p.acc[i];
-            if (!(old < 0.0f)) p.acc[i] = at.decay > 0.0f ? __builtin_fmaf(at.decay, old, mine) : mine;
+            if (!(old < 0.0f)) p.acc[i] = decayed(at, old, mine);
           }
         }
       }
@@ -475,20 +559,28 @@ __global__ __launch_bounds__(kThreads) void attn_sum_join_kernel(Geo g, Attn at,
   if (old < 0.0f) return;
   float sum = 0.0f;
   for (int s = 0; s < row_splits; ++s) sum += part[s * pitch + tr + t];
-  acc[tr + t] = at.decay > 0.0f ? __builtin_fmaf(at.decay, old, sum) : sum;
+  acc[tr + t] = decayed(at, old, sum);
 }
 
 template <typename T, int D, int NT>
 static hipError_t sum_typed(const AttnLaunch& A, const WeightsSpace& w, const void* q, const void* k,
                             const float* lse, float* acc, uint32_t* status) {
   const Geo& g = A.base.geo;
-  SumArgs<T> p{(const T*)q, (const T*)k, lse, acc, ws_ptr<float>(A.base.wsp, w.part), status};
-  const int64_t grid = (int64_t)g.U * std::max(1, w.blocks) * w.row_splits;
-  attn_sum_kernel<T, D, NT, false><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(
-      g, A.at, p, w.blocks, w.row_splits);
-  if (w.row_splits > 1 && g.maxn > 0)
-    attn_sum_join_kernel<<<dim3((g.maxn + kThreads - 1) / kThreads, g.U), kThreads, 0,
-                           A.base.stream>>>(g, A.at, p.part, acc, w.row_splits);
+  float* part = ws_ptr<float>(A.base.wsp, w.part);
+  hipError_t e;
+  if (w.stream_keys) {
+    e = rows_tiles<T, D, true>(A, w, RowArgs<T>{(const T*)q, (const T*)k, acc, lse, nullptr, nullptr,
+                                                status});
+  } else {
+    SumArgs<T> p{(const T*)q, (const T*)k, lse, acc, part, status};
+    attn_sum_kernel<T, D, NT, false>
+        <<<(unsigned)((int64_t)g.U * std::max(1, w.blocks) * w.row_splits), kThreads, 0,
+           A.base.stream>>>(g, A.at, p, w.blocks, w.row_splits);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || w.row_splits == 1 || g.maxn == 0) return e;
+  attn_sum_join_kernel<<<dim3((g.maxn + kThreads - 1) / kThreads, g.U), kThreads, 0, A.base.stream>>>(
+      g, A.at, part, acc, w.row_splits);
   return hipGetLastError();
 }
 
