@@ -25,6 +25,8 @@ constexpr int kKeepRows = 16;
 constexpr int kAttendChunk = 8192;    // tokens per workgroup of the attention: at most,
 constexpr int kAttendChunkMin = 256;  // ... and at least
 constexpr int kAttendBlocks = 512;   // chunks shrink until the grid has this many workgroups
+constexpr int kWideRows = 32;         // more rows than these share K and V through LDS (bf16),
+constexpr int kWideBlocks = 256;      // a workgroup per compute unit
 constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
 // The passes with rows in registers: 16-row tiles per workgroup, at most, and tokens.
 constexpr int kRowTilesBf16 = 8, kRowTilesFp32 = 2;
@@ -152,7 +154,8 @@ constexpr float kLazyMax = 8.0f;
 // ---------------------------------------------------------------------------
 struct AttendSpace {
   int chunk, splits;   // tokens per workgroup, chunks of the longest sequence
-  int mt;              // 16-row tiles per workgroup
+  int mt;              // 16-row tiles per workgroup, or
+  int rw;              // waves of 32 rows that share the cache through LDS (0: none do)
   int row_blocks;
   size_t ml;           // float2 [U][R][splits]     (maximum, sum) of a chunk
   size_t part;         // float  [U][R][splits][D]  its unnormalised output

@@ -135,8 +135,17 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   const int64_t UR = (int64_t)g.U * A.at.R, LHT = (int64_t)g.L * g.H * g.T;
   size_t o = 256;
   w->mt = A.at.R <= 16 ? 1 : 2;
-  w->row_blocks = (A.at.R + 16 * w->mt - 1) / (16 * w->mt);
-  w->chunk = chunk_tokens(g, w->row_blocks, kAttendChunk, kAttendChunkMin, kAttendBlocks);
+  w->rw = !bf16 || A.at.R <= kWideRows ? 0 : A.at.R <= 64 ? 2 : A.at.R <= 128 ? 4 : 8;
+  const int rows = w->rw ? 32 * w->rw : 16 * w->mt;
+  w->row_blocks = (A.at.R + rows - 1) / rows;
+  if (w->rw) {
+    // one round of a workgroup per compute unit, in whole stages of 128 tokens
+    const int64_t per = (LHT * w->row_blocks + kWideBlocks - 1) / kWideBlocks;
+    w->chunk = (int)std::min<int64_t>(std::max<int64_t>((per + 127) / 128 * 128, kAttendChunkMin),
+                                      1 << 20);
+  } else {
+    w->chunk = chunk_tokens(g, w->row_blocks, kAttendChunk, kAttendChunkMin, kAttendBlocks);
+  }
   w->splits = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
   w->keep = A.at.accumulate && A.at.R <= kKeepRows;
   w->lse = o;
