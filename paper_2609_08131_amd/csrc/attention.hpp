@@ -27,6 +27,7 @@ constexpr int kAttendChunkMin = 256;  // ... and at least
 constexpr int kAttendBlocks = 512;   // chunks shrink until the grid has this many workgroups
 constexpr int kWideRows = 32;         // more rows than these share K and V through LDS (bf16),
 constexpr int kWideBlocks = 256;      // a workgroup per compute unit
+constexpr int kJoinFew = 16;           // chunks that one group of threads joins in turn
 constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
 // The passes with rows in registers: 16-row tiles per workgroup, at most, and tokens.
 constexpr int kRowTilesBf16 = 8, kRowTilesFp32 = 2;

@@ -821,7 +821,8 @@ hipError_t launch_attend(const AttnLaunch& A, const AttendSpace& w, const void* 
 }
 
 // ---------------------------------------------------------------------------
-// Second kernel: joins the chunks of each row (a workgroup per row of a unit),
+// Second kernel: joins the chunks of each row (a workgroup per row of a unit, or per
+// 1024 / d rows of few chunks: 8064 rows of 8 chunks 18.9 us at one a workgroup, 8.8 so),
 // and accumulates the weights of kept logits (a workgroup per kJoinTokens
 // tokens of a unit): p = exp2(z - lse) of every row, with lse joined from the
 // chunks again rather than waited for.
@@ -843,22 +844,42 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
                                                                int token_blocks) {
   const int tid = threadIdx.x, S = g.w, R = at.R;
   if ((int)blockIdx.x < rows_grid) {
-    const int u = blockIdx.x / R, r = blockIdx.x - u * R;
-    const Unit un = live_unit(g, u);
-    const int nsp = max(1, (un.n + chunk - 1) / chunk);
-    if (nsp == 1) return;  // written by the first kernel
-    const int64_t ur = (int64_t)u * R + r;
-    const float2* ml = p.ml + ur * splits;
-    __shared__ float red[4];
-    float top = kNoMax;
-    for (int s = tid; s < nsp; s += kThreads) top = fmaxf(top, ml[s].x);
-    top = block_combine(wave_max(top), red, [](float a, float b) { return fmaxf(a, b); });
-    // thread: 4 channels of every NG-th chunk
+    // thread: 4 channels. Few chunks: of a row of its own group of D / 4 threads, all
+    // chunks in turn; many: of every NG-th chunk of the workgroup's one row.
     constexpr int NG = kThreads / (D / 4);
     const int c = tid % (D / 4) * 4, grp = tid / (D / 4);
+    const bool few = splits <= kJoinFew;
+    const int64_t ur = few ? min((int64_t)blockIdx.x * NG + grp, (int64_t)g.U * R - 1) : blockIdx.x;
+    const int u = ur / R, r = ur - (int64_t)u * R;
+    Unit un = decode_unit(g, u);  // (of the group, not of the workgroup)
+    if (g.live) un.n = live_ok(g, un.b, un.n) ? g.live[un.b] : 0;
+    const int nsp = max(1, (un.n + chunk - 1) / chunk);
+    const float2* ml = p.ml + ur * splits;
     const float* part = p.part + ur * splits * D + c;
+    const int head = r / S, pos = r - head * S;
+    T* out = p.out + un.b * at.os + un.l * at.ol + (int64_t)(un.h * g.G + head) * at.oh + pos * at.op;
+    float* lse = p.lse + (((int64_t)un.b * g.L + un.l) * g.Hq + un.h * g.G + head) * S + pos;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.0f;
+    float top = kNoMax, l = 0.0f;
+    if (few) {
+      if (nsp == 1) return;  // written by the first kernel
+      for (int s = 0; s < nsp; ++s) top = fmaxf(top, ml[s].x);
+#pragma unroll 4
+      for (int s = 0; s < nsp; ++s) {
+        const float f = exp2_fast(ml[s].x - top);
+        l += ml[s].y * f;
+        sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * D) * f;
+      }
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[c + e] = (T)(sum[e] * inv);
+      if (p.lse && c == 0) *lse = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
+      return;
+    }
+    if (nsp == 1) return;
+    __shared__ float red[4];
+    for (int s = tid; s < nsp; s += kThreads) top = fmaxf(top, ml[s].x);
+    top = block_combine(wave_max(top), red, [](float a, float b) { return fmaxf(a, b); });
 #pragma unroll 4
     for (int s = grp; s < nsp; s += NG) {
       const float f = exp2_fast(ml[s].x - top);
@@ -876,12 +897,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
         a += so[x][tid];
         b += sl[x];
       }
-      const int head = r / S, pos = r - head * S;
-      p.out[un.b * at.os + un.l * at.ol + (int64_t)(un.h * g.G + head) * at.oh + pos * at.op + tid] =
-          (T)(b == 0.0f ? 0.0f : a / b);
-      if (p.lse && tid == 0)
-        p.lse[(((int64_t)un.b * g.L + un.l) * g.Hq + un.h * g.G + head) * S + pos] =
-            b == 0.0f ? -INFINITY : (top + __log2f(b)) * kLn2;
+      out[tid] = (T)(b == 0.0f ? 0.0f : a / b);
+      if (p.lse && tid == 0) *lse = b == 0.0f ? -INFINITY : (top + __log2f(b)) * kLn2;
     }
     return;
   }
@@ -975,7 +992,8 @@ static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, void* ou
   JoinArgs<T> p{(T*)out, lse, ws_ptr<float2>(ws, w.ml), ws_ptr<float>(ws, w.part),
                 w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
                 w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, acc, acc_draft};
-  const int rows_grid = w.splits > 1 ? g.U * A.at.R : 0;
+  const int64_t UR = (int64_t)g.U * A.at.R, per = w.splits <= kJoinFew ? kThreads / (D / 4) : 1;
+  const int rows_grid = w.splits > 1 ? (int)((UR + per - 1) / per) : 0;
   const int token_blocks = std::max(1, (g.maxn + kJoinTokens - 1) / kJoinTokens);
   const int64_t grid = rows_grid + (w.keep ? (int64_t)g.U * token_blocks : 0);
   attend_join_kernel<T, D><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(
