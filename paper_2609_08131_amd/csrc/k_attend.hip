@@ -73,7 +73,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     rb = x >> 3;
     pair = pair / (8 * row_blocks) * 8 + (x & 7);
   }
-  if (blockIdx.x == 0) write_status(g, p.status);
   if (pair >= g.U * splits) return;
   const int u = pair % g.U, split = pair / g.U;
   const Unit un = live_unit(g, u);
@@ -316,42 +315,42 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
     }
   };
 
+  // The drafted tokens' steps, then the chunk's, in turn over the waves. The next
+  // step's K is requested as soon as this one's has been multiplied, V likewise,
+  // into the same registers: a step's loads are in flight all the time.
   const uint32_t none[MT] = {};
-  const int csteps = (t1 - t0 + W::kStep - 1) / W::kStep;
-  if (wave < csteps) {
-    // The next step's K is requested as soon as this one's has been multiplied, V
-    // likewise, into the same registers: a step's loads are in flight all the time.
-    int r0 = t0 + wave * W::kStep;
-    load_k(kb, g.kst, r0, t1);
-    float a = 0.0f;
-    if constexpr (HIDES) a = load_acc(r0);
-    load_v(vb, g.vst, r0, t1);
-    for (; r0 < t1; r0 += 4 * W::kStep) {
-      const int next = r0 + 4 * W::kStep, rows = min(W::kStep, t1 - r0);
-      uint32_t vis = rows == 32 ? ~0u : (1u << rows) - 1;
-      if constexpr (HIDES) vis &= ~(uint32_t)__ballot(a < 0.0f);
-      step(std::false_type{}, vis, none, r0,
-           [&] {
-             load_k(kb, g.kst, next, t1);
-             if constexpr (HIDES) a = load_acc(next);
-           },
-           [&] { load_v(vb, g.vst, next, t1); });
-    }
+  const T* kdb = p.kd + un.b * at.dks + un.l * at.dkl + un.h * at.dkh;
+  const T* vdb = p.vd + un.b * at.dvs + un.l * at.dvl + un.h * at.dvh;
+  const int dsteps = drafts ? (S + W::kStep - 1) / W::kStep : 0;
+  int r0 = t0 + ((wave - dsteps) & 3) * W::kStep;  // the wave's first step of the chunk
+  {
+    const bool first = wave < dsteps;
+    load_k(first ? kdb : kb, first ? at.dkr : g.kst, first ? wave * W::kStep : r0, first ? S : t1);
+    load_v(first ? vdb : vb, first ? at.dvr : g.vst, first ? wave * W::kStep : r0, first ? S : t1);
   }
-  if (drafts) {
-    const T* kdb = p.kd + un.b * at.dks + un.l * at.dkl + un.h * at.dkh;
-    const T* vdb = p.vd + un.b * at.dvs + un.l * at.dvl + un.h * at.dvh;
-    const int dsteps = (S + W::kStep - 1) / W::kStep;
-    for (int s = (wave + 4 - (csteps & 3)) & 3; s < dsteps; s += 4) {
-      const int r0 = s * W::kStep;
-      load_k(kdb, at.dkr, r0, S);
-      load_v(vdb, at.dvr, r0, S);
-      const int rows = min(W::kStep, S - r0);
-      uint32_t mask[MT];
+  float a = 0.0f;
+  if constexpr (HIDES) a = load_acc(r0);
+  for (int s = wave; s < dsteps; s += 4) {
+    const int d0 = s * W::kStep, rows = min(W::kStep, S - d0);
+    const bool more = s + 4 < dsteps;
+    uint32_t mask[MT];
 #pragma unroll
-      for (int i = 0; i < MT; ++i) mask[i] = row[i] < R ? draft_mask(at, un.b, row[i] % S, S, r0) : 0u;
-      step(std::true_type{}, rows == 32 ? ~0u : (1u << rows) - 1, mask, r0, [] {}, [] {});
-    }
+    for (int i = 0; i < MT; ++i) mask[i] = row[i] < R ? draft_mask(at, un.b, row[i] % S, S, d0) : 0u;
+    const int next = more ? d0 + 4 * W::kStep : r0, end = more ? S : t1;
+    step(std::true_type{}, rows == 32 ? ~0u : (1u << rows) - 1, mask, d0,
+         [&] { load_k(more ? kdb : kb, more ? at.dkr : g.kst, next, end); },
+         [&] { load_v(more ? vdb : vb, more ? at.dvr : g.vst, next, end); });
+  }
+  for (; r0 < t1; r0 += 4 * W::kStep) {
+    const int next = r0 + 4 * W::kStep, rows = min(W::kStep, t1 - r0);
+    uint32_t vis = rows == 32 ? ~0u : (1u << rows) - 1;
+    if constexpr (HIDES) vis &= ~(uint32_t)__ballot(a < 0.0f);
+    step(std::false_type{}, vis, none, r0,
+         [&] {
+           load_k(kb, g.kst, next, t1);
+           if constexpr (HIDES) a = load_acc(next);
+         },
+         [&] { load_v(vb, g.vst, next, t1); });
   }
 
   // Join the waves: rows' maxima and sums first, then the output tile by tile.
@@ -418,6 +417,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
       }
     }
   }
+  if (blockIdx.x == 0) write_status(g, p.status);  // (never one of the empty workgroups)
 }
 
 // ---------------------------------------------------------------------------
@@ -469,7 +469,6 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
     rb = x >> 3;
     pair = pair / (8 * row_blocks) * 8 + (x & 7);
   }
-  if (blockIdx.x == 0) write_status(g, p.status);
   if (pair >= g.U * splits) return;
   const int u = pair % g.U, split = pair / g.U;
   const Unit un = live_unit(g, u);
@@ -765,6 +764,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
             sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
     }
   }
+  if (blockIdx.x == 0) write_status(g, p.status);
 }
 
 template <typename T, int D>

@@ -160,13 +160,13 @@ def _check(fn: str, code: int) -> None:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream) -> int:
     if stream is None:
         stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+    return stream.cuda_stream
 
 
 # ---------------------------------------------------------------------------
@@ -559,6 +559,7 @@ class AttendProblem:
     ws: torch.Tensor
     params: AttentionParams
     seq_offsets: torch.Tensor
+    layout: dict            # name -> (shape, strides, dtype, device) of a run's tensors
 
 
 def prepare_attend(q, k, v, kd, vd, seq_offsets, seq_lens, params: AttentionParams) -> AttendProblem:
@@ -580,47 +581,38 @@ def prepare_attend(q, k, v, kd, vd, seq_offsets, seq_lens, params: AttentionPara
     lse = torch.empty((B, L, Hq, S), dtype=torch.float32, device=k.device)
     acc_draft = torch.empty((B, L, H, S), dtype=torch.float32, device=k.device) \
         if params.accumulate else None
-    return AttendProblem(cfg, batch, attn, out, lse, acc_draft, ws, params, seq_offsets)
+    layout = {n: _layout(t) for n, t in (("q", q), ("k", k), ("v", v), ("kd", kd), ("vd", vd))}
+    layout["acc"] = _acc_layout(k)
+    return AttendProblem(cfg, batch, attn, out, lse, acc_draft, ws, params, seq_offsets, layout)
 
 
-def _expect_strides(prob, **tensors) -> None:
-    """Tensors of a run: laid out as those the problem was prepared with."""
-    for name, (t, shape, strides) in tensors.items():
-        _expect(name, t, shape, _TORCH_DTYPE[prob.cfg.dtype], prob.ws.device, dense=False)
-        if any(n > 1 and x != y for n, x, y in zip(shape, t.stride(), strides)):
-            raise ValueError(f"{name} must have the strides the problem was prepared with")
+def _layout(t: torch.Tensor):
+    return t.shape, t.stride(), t.dtype, t.device
 
 
-def _kv_layout(prob, which: str):
-    c, b = prob.cfg, prob.batch
-    return ((c.num_layers, c.num_kv_heads, b.total_tokens, c.head_dim),
-            tuple(getattr(b, f"{which}_stride_{x}") for x in ("layer", "head", "token")))
+def _expect_layout(prob, name: str, t: torch.Tensor) -> None:
+    """A tensor of a run: laid out as the one the problem was prepared with."""
+    want = prob.layout[name]
+    if t is None:
+        raise ValueError(f"{name} is missing")
+    if (t.shape, t.stride(), t.dtype, t.device) == want:
+        return
+    shape, strides, dtype, device = want
+    _expect(name, t, shape, dtype, device, dense=False)
+    if t.numel() > 0 and any(n > 1 and x != y for n, x, y in zip(shape, t.stride(), strides)):
+        raise ValueError(f"{name} must have the strides the problem was prepared with")
 
 
-def _q_layout(prob):
-    c, b = prob.cfg, prob.batch
-    return ((b.num_seqs, c.num_layers, c.num_q_heads, c.window, c.head_dim),
-            (b.q_stride_seq, b.q_stride_layer, b.q_stride_head, b.q_stride_pos))
-
-
-def _draft_layout(prob, which: str):
-    c, b, a = prob.cfg, prob.batch, prob.attn
-    return ((b.num_seqs, c.num_layers, c.num_kv_heads, c.window, c.head_dim),
-            tuple(getattr(a, f"{which}_stride_{x}") for x in ("seq", "layer", "head", "row")))
-
-
-def _expect_acc(prob, acc) -> None:
-    c, b = prob.cfg, prob.batch
-    _expect("acc", acc, (c.num_layers, c.num_kv_heads, b.total_tokens), torch.float32,
-            prob.ws.device)
+def _acc_layout(k: torch.Tensor):
+    L, H, T, _ = k.shape
+    return torch.Size((L, H, T)), (H * T, T, 1), torch.float32, k.device
 
 
 def run_attend(prob: AttendProblem, q, k, v, kd, vd, acc=None, stream=None) -> None:
-    _expect_strides(prob, q=(q, *_q_layout(prob)), k=(k, *_kv_layout(prob, "k")),
-                    v=(v, *_kv_layout(prob, "v")), kd=(kd, *_draft_layout(prob, "dk")),
-                    vd=(vd, *_draft_layout(prob, "dv")))
-    if acc is not None or prob.attn.accumulate:
-        _expect_acc(prob, acc)
+    for name, t in (("q", q), ("k", k), ("v", v), ("kd", kd), ("vd", vd)):
+        _expect_layout(prob, name, t)
+    if acc is not None or prob.params.accumulate:
+        _expect_layout(prob, "acc", acc)
     attend(prob.cfg, prob.batch, prob.attn, q, k, v, kd, vd, prob.out, prob.lse, acc,
            prob.acc_draft, prob.ws, stream)
 
@@ -636,6 +628,7 @@ class AttnWeightsProblem:
     ws: torch.Tensor
     params: AttentionParams
     seq_offsets: torch.Tensor
+    layout: dict
 
 
 def prepare_attn_weights(q, k, seq_offsets, seq_lens, params: AttentionParams) -> AttnWeightsProblem:
@@ -647,13 +640,14 @@ def prepare_attn_weights(q, k, seq_offsets, seq_lens, params: AttentionParams) -
     attn = _attention(params, B, w, d, k.device)
     ws = _workspace(attn_weights_workspace_size(cfg, batch, attn), k.device)
     lse = torch.empty((B, L, Hq, w), dtype=torch.float32, device=k.device)
-    return AttnWeightsProblem(cfg, batch, attn, lse, ws, params, seq_offsets)
+    layout = {"q": _layout(q), "k": _layout(k), "acc": _acc_layout(k)}
+    return AttnWeightsProblem(cfg, batch, attn, lse, ws, params, seq_offsets, layout)
 
 
 def run_attn_weights(prob: AttnWeightsProblem, q, k, acc, lse=None, stream=None) -> None:
     """lse: the rows' log-sums if they are known (else computed into prob.lse)."""
-    _expect_strides(prob, q=(q, *_q_layout(prob)), k=(k, *_kv_layout(prob, "k")))
-    _expect_acc(prob, acc)
+    for name, t in (("q", q), ("k", k), ("acc", acc)):
+        _expect_layout(prob, name, t)
     if lse is not None:
         _expect("lse", lse, prob.lse.shape, torch.float32, prob.ws.device)
     attn_weights(prob.cfg, prob.batch, prob.attn, q, k, lse, prob.lse if lse is None else None,
@@ -674,6 +668,7 @@ class EvictWeightedProblem:
     ws: torch.Tensor
     live_lens: Optional[torch.Tensor]
     seq_offsets: torch.Tensor
+    layout: dict
 
 
 def prepare_evict_weighted(k, v, seq_offsets, seq_lens, budget: int, protect_last: int = 0,
@@ -703,20 +698,21 @@ def prepare_evict_weighted(k, v, seq_offsets, seq_lens, budget: int, protect_las
     attn = _attention(AttentionParams(live_lens=live_lens), B, 1, d, dev)
     attn.a_stride_seq, attn.a_stride_layer, attn.a_stride_head = acc_out.stride()[:3]
     ws = _workspace(evict_weighted_workspace_size(cfg, batch, attn), dev)
+    layout = {"k": _layout(k), "v": _layout(v), "acc": _acc_layout(k)}
     return EvictWeightedProblem(cfg, batch, attn, idx, k_out, v_out, acc_out, ws, live_lens,
-                                seq_offsets)
+                                seq_offsets, layout)
 
 
 def run_evict_weighted(prob: EvictWeightedProblem, acc, k, v, stream=None) -> None:
-    _expect_strides(prob, k=(k, *_kv_layout(prob, "k")), v=(v, *_kv_layout(prob, "v")))
-    _expect_acc(prob, acc)
+    for name, t in (("acc", acc), ("k", k), ("v", v)):
+        _expect_layout(prob, name, t)
     evict_weighted(prob.cfg, prob.batch, prob.attn, acc, k, v, prob.idx, prob.k_out, prob.v_out,
                    prob.acc_out, stream)
 
 
 def run_evict_weighted_slots(prob: EvictWeightedProblem, acc, slots, stream=None) -> None:
     """slots: int32 [B][L][H_kv][cap], cap >= max_seq_len - budget (alloc_slots); acc is updated."""
-    _expect_acc(prob, acc)
+    _expect_layout(prob, "acc", acc)
     _expect("slots", slots, (*prob.idx.shape[:3], slots.shape[-1]), torch.int32, prob.ws.device)
     evict_weighted_slots(prob.cfg, prob.batch, prob.attn, acc, slots, prob.ws, stream)
 
