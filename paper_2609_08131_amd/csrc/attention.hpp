@@ -22,12 +22,14 @@ constexpr int kMaxDraft = 512;        // rows per query head jacap_attend takes
 // token written, then read) to accumulate from; more rows, and their keys are
 // read again (256 bytes a token at d = 128, bf16) and multiplied again.
 constexpr int kKeepRows = 16;
-constexpr int kAttendChunk = 8192;    // tokens per workgroup of the attention: at most,
-constexpr int kAttendChunkMin = 256;  // ... and at least
-constexpr int kAttendBlocks = 512;   // chunks shrink until the grid has this many workgroups
+constexpr int kSpans = 512;           // workgroups the attention of few rows is cut into, of
+constexpr int kSpanMin = 256;         // ... at least this many tokens
+constexpr int kUnitGroups = 4;        // what beginning and ending a unit costs, in groups of 4 steps
+constexpr int kWideChunkMin = 256;    // tokens per workgroup of many rows, at least
 constexpr int kWideRows = 32;         // more rows than these share K and V through LDS (bf16),
 constexpr int kWideBlocks = 256;      // a workgroup per compute unit
-constexpr int kJoinFew = 16;           // chunks that one group of threads joins in turn
+constexpr int kJoinFew = 16;           // pieces of a row that one group of threads joins in turn
+constexpr int kJoinRows = 1024;        // rows of a batch up to which a workgroup joins one
 constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
 // The passes with rows in registers: 16-row tiles per workgroup, at most, and tokens.
 constexpr int kRowTilesBf16 = 8, kRowTilesFp32 = 2;
@@ -154,12 +156,15 @@ constexpr float kLazyMax = 8.0f;
 // Workspaces (byte offsets; the status word at 0) and launchers
 // ---------------------------------------------------------------------------
 struct AttendSpace {
-  int chunk, splits;   // tokens per workgroup, chunks of the longest sequence
-  int mt;              // 16-row tiles per workgroup, or
-  int rw;              // waves of 32 rows that share the cache through LDS (0: none do)
+  int mt;              // 16-row tiles per workgroup,
+  int spans;           // ... and workgroups; or
+  int rw;              // waves of 32 rows that share the cache through LDS (0: none do),
+  int chunk, splits;   // ... with tokens per workgroup, chunks of the longest sequence
   int row_blocks;
-  size_t ml;           // float2 [U][R][splits]     (maximum, sum) of a chunk
-  size_t part;         // float  [U][R][splits][D]  its unnormalised output
+  size_t before;       // int32 [B + 1]             groups of tokens before each sequence
+  size_t ml;           // float2 [pieces]           (maximum, sum) of a row's piece
+  size_t part;         // float  [pieces][D]        its unnormalised output; the pieces:
+                       // [2 spans][16 mt], or [U][R][splits]
   size_t lse;          // float  [U][R]
   size_t z;            // float  [L][H][tiles][R][16] kept logits (accumulating from few rows)
   size_t zd;           // float  [U][R][S]          ... and the drafted tokens'

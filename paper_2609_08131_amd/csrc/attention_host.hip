@@ -138,22 +138,31 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   w->rw = !bf16 || A.at.R <= kWideRows ? 0 : A.at.R <= 64 ? 2 : A.at.R <= 128 ? 4 : 8;
   const int rows = w->rw ? 32 * w->rw : 16 * w->mt;
   w->row_blocks = (A.at.R + rows - 1) / rows;
+  w->spans = 0;
+  w->chunk = w->splits = 1;
+  int64_t pieces;
   if (w->rw) {
     // one round of a workgroup per compute unit, in whole stages of 128 tokens
     const int64_t per = (LHT * w->row_blocks + kWideBlocks - 1) / kWideBlocks;
-    w->chunk = (int)std::min<int64_t>(std::max<int64_t>((per + 127) / 128 * 128, kAttendChunkMin),
+    w->chunk = (int)std::min<int64_t>(std::max<int64_t>((per + 127) / 128 * 128, kWideChunkMin),
                                       1 << 20);
+    w->splits = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
+    pieces = UR * w->splits;
   } else {
-    w->chunk = chunk_tokens(g, w->row_blocks, kAttendChunk, kAttendChunkMin, kAttendBlocks);
+    // no more spans than there can be work for
+    const int64_t most = (LHT / kSpanMin + (int64_t)g.U * (1 + kUnitGroups)) * w->row_blocks;
+    w->spans = (int)std::min<int64_t>(kSpans, most);
+    pieces = 2 * (int64_t)w->spans * rows;
   }
-  w->splits = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
   w->keep = A.at.accumulate && A.at.R <= kKeepRows;
+  w->before = o;
+  o = align256(o + 4 * ((size_t)g.B + 1));
   w->lse = o;
   o = align256(o + 4 * (size_t)UR);
   w->ml = o;
-  o = align256(o + 8 * (size_t)UR * w->splits);
+  o = align256(o + 8 * (size_t)pieces);
   w->part = o;
-  if (w->splits > 1) o = align256(o + 4 * (size_t)UR * w->splits * g.D);
+  o = align256(o + 4 * (size_t)pieces * g.D);
   w->z = o;
   if (w->keep) o = align256(o + 4 * (size_t)g.L * g.H * (g.T / 16 + g.B + 1) * 16 * A.at.R);
   w->zd = o;
@@ -161,10 +170,12 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   *sum = WeightsSpace{};
   if (A.at.accumulate && !w->keep) layout_sum(g, A.at, bf16, sum, &o);
   w->total = o;
-  const int64_t pairs = (int64_t)g.U * w->splits + 8;
   const int64_t token_blocks = g.maxn / kJoinTokens + 1;
-  if (pairs * w->row_blocks > kMaxGrid || UR + g.U * token_blocks > kMaxGrid ||
-      !sum_grid_ok(g, *sum))
+  // 32-bit counts of groups (of at least 64 tokens) and of pieces
+  const int64_t groups =
+      (int64_t)g.L * g.H * w->row_blocks * (g.T / 64 + (int64_t)g.B * (1 + kUnitGroups));
+  if (((int64_t)g.U * w->splits + 8) * w->row_blocks > kMaxGrid || UR + g.U * token_blocks > kMaxGrid ||
+      groups > INT32_MAX / 2 || pieces > INT32_MAX || !sum_grid_ok(g, *sum))
     return JACAP_ERR_UNSUPPORTED;
   return JACAP_OK;
 }
@@ -220,7 +231,7 @@ jacap_status jacap_attend(const jacap_config* cfg, const jacap_batch* batch,
     return JACAP_ERR_INVALID_ARG;
   if (attn->accumulate && !acc && batch->total_tokens > 0) return JACAP_ERR_INVALID_ARG;
   const bool sums = attn->accumulate && !w.keep;  // a pass of its own, from the rows' lse
-  float* ls = lse ? lse : sums ? ws_ptr<float>(A.base.wsp, w.lse) : nullptr;
+  float* ls = lse ? lse : attn->accumulate ? ws_ptr<float>(A.base.wsp, w.lse) : nullptr;
   {
     TimedPhase tp(A.base.stream, JACAP_PHASE_ATTEND);
     JACAP_TRY(launch_attend(A, w, q, k, v, kd, vd, out, ls, acc));

@@ -4,10 +4,10 @@
 //   z_ri = scale q_r . k_i,  lse_r = log sum exp(z_r.),  out_r = sum exp(z_r. - lse_r) v
 //
 // One pass over K and V with the running maximum and sum of a softmax. A
-// workgroup takes one unit, 16 MT of its R = G S rows and one chunk of its
-// tokens; its four waves take the chunk's steps in turn, each with a softmax
-// of its own, and no barrier before the chunk's end, where they are joined
-// in LDS. The chunks of long sequences are joined by a second kernel.
+// workgroup takes 16 MT of the R = G S rows of a unit and a stretch of its
+// tokens; its four waves take the stretch's steps in turn, each with a softmax
+// of its own, and no barrier before the stretch's end, where they are joined
+// in LDS. The stretches of long sequences are joined by a second kernel.
 //
 // P V without a transpose in LDS: the second product is also formed
 // transposed, O^T = V^T P^T, and a lane's logits (query row m, tokens 4 q ..
@@ -36,6 +36,7 @@ struct AttendArgs {
   float* part;
   float *z, *zd;     // kept logits, or null
   uint32_t* status;
+  int32_t* before;   // groups before each sequence
 };
 
 // What the accumulators do in a call, apart in the code: a load or store that
@@ -57,30 +58,120 @@ __device__ __forceinline__ uint32_t draft_mask(const Attn& at, int b, int pos, i
   return last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1u;
 }
 
+// How attend_kernel's work is cut: every unit (and row block of it: L H row_blocks
+// of them per sequence, side by side) is a run of groups of 4 steps, one step per
+// wave, at least one group (the drafted tokens go with the last), and kUnitGroups
+// empty ones after them, the cost of beginning and ending a unit. The runs of all
+// units in order are cut into spans of `quantum` groups, one per workgroup, whatever
+// the sequences' lengths are when the kernel runs. A workgroup's span begins in one
+// unit and ends in one; what it holds of a unit that it shares with others is
+// written apart, as piece 2 w (of the unit it begins in) or 2 w + 1, and joined later.
+// Against chunks of equal size (16 sequences of 4096 to 32768 tokens, 600 chunks of
+// 4096 on 512 places: 206 us) every place has the same work: 176 us.
+template <typename T, int D>
+constexpr int kGroup = 4 * Row<T, D>::kStep;
+
+__device__ __forceinline__ int real_groups(int n, int group) { return max(1, (n + group - 1) / group); }
+__device__ __forceinline__ int span_quantum(int groups, int blocks, int group) {
+  return max(kSpanMin / group, (groups + blocks - 1) / blocks);
+}
+// Where piece j of a unit whose groups begin at `start` lies.
+__device__ __forceinline__ int64_t piece_of(int start, int quantum, int j) {
+  const int w = start / quantum;
+  return 2 * (int64_t)(w + j) + (j == 0 && start != w * quantum);
+}
+// A sequence's first cache row and current length.
+__device__ __forceinline__ int2 sequence_rows(const Geo& g, int b) {
+  const int32_t a = g.seq_off[b], e = g.seq_off[b + 1];
+  int n = offsets_ok(g, a, e) ? e - a : 0;
+  if (g.live) n = live_ok(g, b, n) ? g.live[b] : 0;
+  return int2{a, n};
+}
+// Inclusive scan over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // last lane of rows 0, 2 to 1, 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2, 3
+  return v;
+}
+
+template <typename T>
+struct AttendParams {
+  Geo g;
+  Attn at;
+  AttendArgs<T> p;
+  int row_blocks;
+};
+
 template <typename T, int D, int MT, Mode MODE>
-__global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, AttendArgs<T> p,
-                                                          int chunk, int splits, int row_blocks) {
+__global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> params) {
   using W = Row<T, D>;
   constexpr int NT = W::kTiles, NP = W::kPieces, NL = W::kVLoads, VW = W::kVWords;
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Workgroup -> (unit, chunk, row block): chunk-major; the row blocks of a
-  // (unit, chunk) read the same K and V, and run 8 apart (same XCD, see
-  // grid_unit_chunk_at).
-  int pair = blockIdx.x, rb = 0;
-  if (row_blocks > 1) {
-    const int x = pair % (8 * row_blocks);
-    rb = x >> 3;
-    pair = pair / (8 * row_blocks) * 8 + (x & 7);
+  constexpr int GROUP = kGroup<T, D>;
+  const int per_seq = params.g.L * params.g.H * params.row_blocks;  // units and row blocks of one
+  __shared__ float sm[4][16 * MT], sl[4][16 * MT];
+  __shared__ __align__(16) float red[4][16][D + 4];
+  // The sequences' rows, 64 sequences at a time in the lanes; the first ones are kept.
+  const int B = params.g.B;
+  auto rows64 = [&](int b0) { return b0 + lane < B ? sequence_rows(params.g, b0 + lane) : int2{0, -1}; };
+  auto groups64 = [&](const int2& x) { return x.y < 0 ? 0 : real_groups(x.y, GROUP) + kUnitGroups; };
+  int2 held = rows64(0);
+  int held_b = 0;
+  int seq_groups = 0;
+  for (int b0 = 0; b0 < B; b0 += 64)
+    seq_groups += __builtin_amdgcn_readlane(wave_scan(groups64(b0 == 0 ? held : rows64(b0))), 63);
+  const int total = seq_groups * per_seq;
+  const int quantum = span_quantum(total, gridDim.x, GROUP);
+  int at_group = blockIdx.x * quantum;
+  const int end_group = min(total, at_group + quantum);
+  // the sequence of the span's first group, and the groups before it (of one unit each)
+  int b = 0, before = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    if (b0 > 0) held = rows64(held_b = b0);
+    const int c = groups64(held), incl = before + wave_scan(c);
+    const uint64_t past = __ballot(incl * per_seq > at_group);
+    if (past) {
+      const int j = __builtin_ctzll(past);
+      b = b0 + j;
+      before = __builtin_amdgcn_readlane(incl - c, j);
+      break;
+    }
+    before = __builtin_amdgcn_readlane(incl, 63);
   }
-  if (pair >= g.U * splits) return;
-  const int u = pair % g.U, split = pair / g.U;
-  const Unit un = live_unit(g, u);
-  const int S = g.w, R = at.R;
-  const int nsp = max(1, (un.n + chunk - 1) / chunk);
-  if (split >= nsp) return;
-  const int t0 = split * chunk, t1 = min(un.n, t0 + chunk);
-  const bool drafts = split == nsp - 1;  // the last chunk takes the drafted tokens
+  while (at_group < end_group) {
+  // The parameters are read again for each unit: kept in registers over the loop,
+  // they would not fit (200 scalar registers spilled to vector lanes).
+  auto args = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(args));
+  const AttendParams<T>& again = *(const AttendParams<T>*)args;
+  const Geo& g = again.g;
+  const Attn& at = again.at;
+  const AttendArgs<T>& p = again.p;
+  const int row_blocks = again.row_blocks, S = g.w, R = at.R;
+  int n, c;  // the sequence's length and groups
+  for (;;) {
+    if (b >= held_b + 64) held = rows64(held_b = b);
+    n = __builtin_amdgcn_readlane(held.y, b - held_b);
+    c = real_groups(n, GROUP);
+    if (at_group < (before + c + kUnitGroups) * per_seq) break;
+    before += c + kUnitGroups;
+    ++b;
+  }
+  const int run = c + kUnitGroups, in_seq = at_group - before * per_seq;
+  const int vu = in_seq / run, from = in_seq - vu * run, len = min(run - from, end_group - at_group);
+  const int first_group = at_group;
+  at_group += len;
+  if (from >= c) continue;
+  const int rb = vu % row_blocks, lh = vu / row_blocks, u = b * g.L * g.H + lh;
+  const Unit un = {b, lh / g.H, lh % g.H, 0, __builtin_amdgcn_readlane(held.x, b - held_b), n};
+  const bool drafts = from + len >= c, whole = from == 0 && drafts;
+  const int t0 = from * GROUP, t1 = min(n, (from + len) * GROUP);
+  const int64_t piece = 2 * (int64_t)blockIdx.x + (first_group != (int)blockIdx.x * quantum);
 
   // The query rows (lane: row m of each tile).
   uint4 qf[MT][NP];
@@ -354,8 +445,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
   }
 
   // Join the waves: rows' maxima and sums first, then the output tile by tile.
-  __shared__ float sm[4][16 * MT], sl[4][16 * MT];
-  __shared__ __align__(16) float red[4][16][D + 4];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     l[i] += __shfl_xor(l[i], 16);
@@ -398,9 +487,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
       for (int c = 0; c < PER; ++c) val[c] += red[x][jr][jc + c];
     }
     if (r < R) {
-      const int64_t ur = (int64_t)u * R + r;
-      if ((tid & 15) == 0 && (splits > 1 || MODE == kKeeps)) p.ml[ur * splits + split] = float2{jt, sum};
-      if (nsp == 1) {
+      if (whole) {
         const int head = r / S, pos = r - head * S;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         T* dst = p.out + un.b * at.os + un.l * at.ol + (int64_t)(un.h * g.G + head) * at.oh +
@@ -411,13 +498,29 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(Geo g, Attn at, Att
           p.lse[(((int64_t)un.b * g.L + un.l) * g.Hq + un.h * g.G + head) * S + pos] =
               sum == 0.0f ? -INFINITY : (jt + __log2f(sum)) * kLn2;
       } else {
-        float* dst = p.part + (ur * splits + split) * D + jc;
+        const int64_t pr = piece * (16 * MT) + 16 * i + jr;
+        if ((tid & 15) == 0) p.ml[pr] = float2{jt, sum};
+        float* dst = p.part + pr * D + jc;
 #pragma unroll
         for (int c = 0; c < PER; ++c) dst[c] = val[c];
       }
     }
   }
-  if (blockIdx.x == 0) write_status(g, p.status);  // (never one of the empty workgroups)
+  __syncthreads();  // the joined tiles are read before the next unit's are written
+  }
+  if (blockIdx.x == 0) {
+    // for the join: the groups before each sequence
+    if (wave == 0) {
+      int sum = 0;
+      for (int b0 = 0; b0 < B; b0 += 64) {
+        const int incl = sum + wave_scan(groups64(rows64(b0)));
+        if (b0 + lane < B) params.p.before[b0 + lane + 1] = incl;
+        sum = __builtin_amdgcn_readlane(incl, 63);
+      }
+      if (lane == 0) params.p.before[0] = 0;
+    }
+    write_status(params.g, params.p.status);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -776,14 +879,15 @@ static hipError_t attend_typed(const AttnLaunch& A, const AttendSpace& w, const 
   AttendArgs<T> p{(const T*)q, (const T*)k, (const T*)v, (const T*)kd, (const T*)vd, (T*)out, lse,
                   acc, ws_ptr<float2>(ws, w.ml), ws_ptr<float>(ws, w.part),
                   w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
-                  w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, ws_ptr<uint32_t>(ws, 0)};
-  const int64_t pairs = (int64_t)g.U * w.splits;
-  const int64_t grid = w.row_blocks > 1 ? (pairs + 7) / 8 * 8 * w.row_blocks : pairs;
+                  w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, ws_ptr<uint32_t>(ws, 0),
+                  ws_ptr<int32_t>(ws, w.before)};
   auto go = [&](auto kern) {
-    kern<<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, w.chunk, w.splits, w.row_blocks);
+    kern<<<w.spans, kThreads, 0, A.base.stream>>>(AttendParams<T>{g, A.at, p, w.row_blocks});
   };
   if constexpr (sizeof(T) == 2) {
     if (w.rw > 0) {
+      const int64_t pairs = (int64_t)g.U * w.splits;
+      const int64_t grid = w.row_blocks > 1 ? (pairs + 7) / 8 * 8 * w.row_blocks : pairs;
       auto wide = [&](auto kern, int lds) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -830,62 +934,85 @@ hipError_t launch_attend(const AttnLaunch& A, const AttendSpace& w, const void* 
 template <typename T>
 struct JoinArgs {
   T* out;
-  float* lse;             // or null
+  float* lse;             // or null (not with kept logits)
   const float2* ml;
   const float* part;
+  const int32_t* before;
   const float *z, *zd;    // or null
   float* acc;
   float* acc_draft;       // or null
 };
 
+// Where a row's pieces lie: `n` of them (1: the first kernel wrote the result), each
+// a (maximum, sum) and an unnormalised output; piece j at row(j).
+struct Pieces {
+  int n, start, quantum, rows, in_block;  // spans; quantum 0: chunks, start the row's first
+  __device__ __forceinline__ int64_t row(int j) const {
+    return quantum ? piece_of(start, quantum, j) * rows + in_block : (int64_t)start + j;
+  }
+};
+// spans > 0: attend_kernel's, in groups of `group` tokens and blocks of `rows` rows;
+// else attend_wide_kernel's chunks.
+struct JoinGeo {
+  int chunk, splits, spans, group, rows, row_blocks;
+};
+__device__ __forceinline__ Pieces pieces_of(const Geo& g, const JoinGeo& j, const int32_t* before,
+                                            const Unit& un, int u, int r, int R) {
+  if (j.spans == 0)
+    return {max(1, (un.n + j.chunk - 1) / j.chunk), (int)(((int64_t)u * R + r) * j.splits), 0, 0, 0};
+  const int per_seq = g.L * g.H * j.row_blocks;
+  const int q = span_quantum(before[g.B] * per_seq, j.spans, j.group);
+  const int run = before[un.b + 1] - before[un.b], c = run - kUnitGroups;
+  const int start = before[un.b] * per_seq + ((un.l * g.H + un.h) * j.row_blocks + r / j.rows) * run;
+  return {(start + c - 1) / q - start / q + 1, start, q, j.rows, r % j.rows};
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, JoinArgs<T> p,
-                                                               int chunk, int splits, int rows_grid,
+                                                               JoinGeo jg, int few, int rows_grid,
                                                                int token_blocks) {
   const int tid = threadIdx.x, S = g.w, R = at.R;
   if ((int)blockIdx.x < rows_grid) {
-    // thread: 4 channels. Few chunks: of a row of its own group of D / 4 threads, all
-    // chunks in turn; many: of every NG-th chunk of the workgroup's one row.
+    // thread: 4 channels. Few pieces: of a row of its own group of D / 4 threads, all
+    // pieces in turn; many: of every NG-th piece of the workgroup's one row.
     constexpr int NG = kThreads / (D / 4);
     const int c = tid % (D / 4) * 4, grp = tid / (D / 4);
-    const bool few = splits <= kJoinFew;
     const int64_t ur = few ? min((int64_t)blockIdx.x * NG + grp, (int64_t)g.U * R - 1) : blockIdx.x;
     const int u = ur / R, r = ur - (int64_t)u * R;
-    Unit un = decode_unit(g, u);  // (of the group, not of the workgroup)
-    if (g.live) un.n = live_ok(g, un.b, un.n) ? g.live[un.b] : 0;
-    const int nsp = max(1, (un.n + chunk - 1) / chunk);
-    const float2* ml = p.ml + ur * splits;
-    const float* part = p.part + ur * splits * D + c;
+    Unit un{u / (g.L * g.H), u / g.H % g.L, u % g.H};  // (of the group, not of the workgroup)
+    if (jg.spans == 0) un.n = sequence_rows(g, un.b).y;
+    const Pieces pc = pieces_of(g, jg, p.before, un, u, r, R);
+    // one piece: written by the first kernel (threads of a wave may hold different rows)
+    if (pc.n == 1) return;
     const int head = r / S, pos = r - head * S;
     T* out = p.out + un.b * at.os + un.l * at.ol + (int64_t)(un.h * g.G + head) * at.oh + pos * at.op;
     float* lse = p.lse + (((int64_t)un.b * g.L + un.l) * g.Hq + un.h * g.G + head) * S + pos;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     float top = kNoMax, l = 0.0f;
+    auto add = [&](int s) {
+      const int64_t at_row = pc.row(s);
+      const float2 ml = p.ml[at_row];
+      const float f = exp2_fast(ml.x - top);
+      l += ml.y * f;
+      sum += *reinterpret_cast<const f32x4*>(p.part + at_row * D + c) * f;
+    };
     if (few) {
-      if (nsp == 1) return;  // written by the first kernel
-      for (int s = 0; s < nsp; ++s) top = fmaxf(top, ml[s].x);
-#pragma unroll 4
-      for (int s = 0; s < nsp; ++s) {
-        const float f = exp2_fast(ml[s].x - top);
-        l += ml[s].y * f;
-        sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * D) * f;
-      }
+      for (int s = c / 4; s < pc.n; s += D / 4) top = fmaxf(top, p.ml[pc.row(s)].x);
+#pragma unroll
+      for (int x = D / 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+#pragma unroll 8
+      for (int s = 0; s < pc.n; ++s) add(s);
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
       for (int e = 0; e < 4; ++e) out[c + e] = (T)(sum[e] * inv);
       if (p.lse && c == 0) *lse = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
       return;
     }
-    if (nsp == 1) return;
     __shared__ float red[4];
-    for (int s = tid; s < nsp; s += kThreads) top = fmaxf(top, ml[s].x);
+    for (int s = tid; s < pc.n; s += kThreads) top = fmaxf(top, p.ml[pc.row(s)].x);
     top = block_combine(wave_max(top), red, [](float a, float b) { return fmaxf(a, b); });
 #pragma unroll 4
-    for (int s = grp; s < nsp; s += NG) {
-      const float f = exp2_fast(ml[s].x - top);
-      l += ml[s].y * f;
-      sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * D) * f;
-    }
+    for (int s = grp; s < pc.n; s += NG) add(s);
     __shared__ __align__(16) float so[NG][D];
     __shared__ float sl[NG];
     *reinterpret_cast<f32x4*>(&so[grp][c]) = sum;
@@ -907,7 +1034,6 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   const Unit un = live_unit(g, u);
   const int t0 = blk * kJoinTokens;
   if (t0 >= un.n && blk > 0) return;
-  const int nsp = max(1, (un.n + chunk - 1) / chunk);
   // The entries and the first rows' logits are requested before the rows' lse is
   // joined. Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
   const int64_t tr = token_row(g, un) + t0;
@@ -927,15 +1053,23 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   }
   __shared__ float slse[kKeepRows], sw[kKeepRows];
   {
-    // 16 threads per row
-    const int r = tid >> 4;
+    // 16 threads per row; a row of one piece has its lse already, as a sum of 1
+    const int r = tid >> 4, rc = min(r, R - 1);
+    const Pieces pc = pieces_of(g, jg, p.before, un, u, rc, R);
     float top = kNoMax, l = 0.0f;
-    const float2* ml = p.ml + ((int64_t)u * R + min(r, R - 1)) * splits;
-    for (int s = tid & 15; s < nsp; s += 16) {
-      const float2 c = ml[s];
-      const float now = fmaxf(top, c.x);
-      l = l * exp2_fast(top - now) + c.y * exp2_fast(c.x - now);
-      top = now;
+    if (pc.n == 1) {
+      const float ls = p.lse[(int64_t)u * R + rc];
+      if ((tid & 15) == 0 && ls != -INFINITY) {
+        top = ls * kLog2e;
+        l = 1.0f;
+      }
+    } else {
+      for (int s = tid & 15; s < pc.n; s += 16) {
+        const float2 c = p.ml[pc.row(s)];
+        const float now = fmaxf(top, c.x);
+        l = l * exp2_fast(top - now) + c.y * exp2_fast(c.x - now);
+        top = now;
+      }
     }
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) {
@@ -982,24 +1116,31 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   }
 }
 
-bool attend_joins(const AttnLaunch& A, const AttendSpace& w) { return w.splits > 1 || w.keep; }
-
 template <typename T, int D>
 static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, void* out, float* lse,
                              float* acc, float* acc_draft) {
   const Geo& g = A.base.geo;
   char* ws = A.base.wsp;
   JoinArgs<T> p{(T*)out, lse, ws_ptr<float2>(ws, w.ml), ws_ptr<float>(ws, w.part),
-                w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
+                ws_ptr<int32_t>(ws, w.before), w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
                 w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, acc, acc_draft};
-  const int64_t UR = (int64_t)g.U * A.at.R, per = w.splits <= kJoinFew ? kThreads / (D / 4) : 1;
-  const int rows_grid = w.splits > 1 ? (int)((UR + per - 1) / per) : 0;
+  const bool wide = w.rw > 0;
+  const JoinGeo jg{w.chunk, w.splits, wide ? 0 : w.spans, kGroup<T, D>, 16 * w.mt, w.row_blocks};
+  // Spans of a batch of many rows hold many units each, so a row has few pieces; of
+  // few rows (at most a workgroup's worth per compute unit), as many as there are spans.
+  const int64_t UR = (int64_t)g.U * A.at.R;
+  const int few = wide ? w.splits <= kJoinFew : UR > kJoinRows;
+  const int64_t per = few ? kThreads / (D / 4) : 1;
+  const int rows_grid = wide && w.splits == 1 ? 0 : (int)((UR + per - 1) / per);
   const int token_blocks = std::max(1, (g.maxn + kJoinTokens - 1) / kJoinTokens);
   const int64_t grid = rows_grid + (w.keep ? (int64_t)g.U * token_blocks : 0);
-  attend_join_kernel<T, D><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(
-      g, A.at, p, w.chunk, w.splits, rows_grid, token_blocks);
+  attend_join_kernel<T, D><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, jg, few, rows_grid,
+                                                                           token_blocks);
   return hipGetLastError();
 }
+
+// (a wide batch of one chunk per unit is written by its kernel)
+bool attend_joins(const AttnLaunch& A, const AttendSpace& w) { return w.rw == 0 || w.splits > 1; }
 
 hipError_t launch_attend_join(const AttnLaunch& A, const AttendSpace& w, void* out, float* lse,
                               float* acc, float* acc_draft) {
