@@ -116,6 +116,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> par
   const int per_seq = params.g.L * params.g.H * params.row_blocks;  // units and row blocks of one
   __shared__ float sm[4][16 * MT], sl[4][16 * MT];
   __shared__ __align__(16) float red[4][16][D + 4];
+  {
+    // The parameters' cache lines, requested together: the loop reads them piece by
+    // piece, each piece's first read a miss of its own (8 units of 8192 tokens: 12 us, 11 so).
+    auto line = [](int i) { return ((const uint32_t*)__builtin_amdgcn_kernarg_segment_ptr())[16 * i]; };
+    static_assert(sizeof(AttendParams<T>) > 6 * 64 && sizeof(AttendParams<T>) <= 7 * 64, "lines");
+    asm volatile("" ::"s"(line(0)), "s"(line(1)), "s"(line(2)), "s"(line(3)), "s"(line(4)), "s"(line(5)),
+                 "s"(line(6)));
+  }
   // The sequences' rows, 64 sequences at a time in the lanes; the first ones are kept.
   const int B = params.g.B;
   auto rows64 = [&](int b0) { return b0 + lane < B ? sequence_rows(params.g, b0 + lane) : int2{0, -1}; };
@@ -167,7 +175,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> par
   const int first_group = at_group;
   at_group += len;
   if (from >= c) continue;
-  const int rb = vu % row_blocks, lh = vu / row_blocks, u = b * g.L * g.H + lh;
+  const int lh = row_blocks == 1 ? vu : vu / row_blocks, rb = vu - lh * row_blocks;
+  const int u = b * g.L * g.H + lh;
   const Unit un = {b, lh / g.H, lh % g.H, 0, __builtin_amdgcn_readlane(held.x, b - held_b), n};
   const bool drafts = from + len >= c, whole = from == 0 && drafts;
   const int t0 = from * GROUP, t1 = min(n, (from + len) * GROUP);
@@ -508,7 +517,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> par
   }
   __syncthreads();  // the joined tiles are read before the next unit's are written
   }
-  if (blockIdx.x == 0) {
+  if (blockIdx.x == gridDim.x - 1) {  // (its span is the shortest, if it has one)
     // for the join: the groups before each sequence
     if (wave == 0) {
       int sum = 0;
@@ -1034,13 +1043,12 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   const Unit un = live_unit(g, u);
   const int t0 = blk * kJoinTokens;
   if (t0 >= un.n && blk > 0) return;
-  // The entries and the first rows' logits are requested before the rows' lse is
-  // joined. Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
+  // The entries and the rows' logits are requested before the rows' lse is joined. Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
   const int64_t tr = token_row(g, un) + t0;
   const float* z = p.z + keep_at(g, un, R, t0 / 16 + tid / 16) + tid % 16;
   const int left = un.n - t0;
-  constexpr int PER = kJoinTokens / kThreads, FIRST = 4;
-  float old[PER], sum[PER], y[FIRST][PER];
+  constexpr int PER = kJoinTokens / kThreads;
+  float old[PER], sum[PER], y[kKeepRows][PER];
   auto logit = [&](int r, int x) {
     return tid + x * kThreads < left ? z[x * (kThreads / 16) * R * 16 + r * 16] : -INFINITY;
   };
@@ -1049,7 +1057,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     old[x] = tid + x * kThreads < left ? p.acc[tr + tid + x * kThreads] : -1.0f;
     sum[x] = 0.0f;
 #pragma unroll
-    for (int r = 0; r < FIRST; ++r) y[r][x] = r < R ? logit(r, x) : -INFINITY;
+    for (int r = 0; r < kKeepRows; ++r)
+      if (r < R) y[r][x] = logit(r, x);
   }
   __shared__ float slse[kKeepRows], sw[kKeepRows];
   {
@@ -1093,15 +1102,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
       for (int x = 0; x < PER; ++x) sum[x] = __builtin_fmaf(w, exp2_fast(v[x] - ls), sum[x]);
   };
 #pragma unroll
-  for (int r = 0; r < FIRST; ++r)
+  for (int r = 0; r < kKeepRows; ++r)
     if (r < R) add(r, y[r]);
-#pragma unroll 4
-  for (int r = FIRST; r < R; ++r) {
-    float v[PER];
-#pragma unroll
-    for (int x = 0; x < PER; ++x) v[x] = logit(r, x);
-    add(r, v);
-  }
 #pragma unroll
   for (int x = 0; x < PER; ++x)
     if (tid + x * kThreads < left && !(old[x] < 0.0f))

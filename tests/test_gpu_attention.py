@@ -155,6 +155,32 @@ def test_attend_long(jacap, dtype, S, lens):
     check_attend(c, prob, acc, True, True, decay=0.0, row_weight=rw)
 
 
+@pytest.mark.parametrize("dtype,S,G", [(BF, 1, 2), (F32, 1, 1), (BF, 20, 1), (F32, 24, 2), (BF, 40, 1)])
+def test_attend_many_sequences(jacap, dtype, S, G):
+    """More sequences than a wave has lanes, most of them short, one long: the spans'
+    search, units that begin and end inside a span, rows of several blocks (fp32)."""
+    gen = torch.Generator().manual_seed(11)
+    lens = [int(x) for x in torch.randint(0, 90, (150,), generator=gen)]
+    lens[3], lens[70], lens[149] = 2000, 9000, 700
+    c = Case(lens, S, dtype, 64, H=1, G=G, holes=0.1, spare=2, tree="tree" if S > 1 else None, seed=8)
+    prob, acc = run_attend(jacap, c, True, True)
+    check_attend(c, prob, acc, True, True)
+
+
+@pytest.mark.parametrize("lens", [[0], [0, 0, 0], [1], [0, 200000, 0, 5]])
+def test_attend_lengths_of_nothing_beside_long_ones(jacap, lens):
+    c = Case(lens, 1, BF, 64, H=2, G=1, seed=14)
+    prob, acc = run_attend(jacap, c, False, True)
+    check_attend(c, prob, acc, False, True)
+
+
+def test_capacity_far_above_the_lengths(jacap):
+    """Caches with room for far more than they hold."""
+    c = Case([900, 3, 0, 257], 1, BF, 128, H=2, G=4, spare=30000, holes=0.05, seed=15)
+    prob, acc = run_attend(jacap, c, True, True)
+    check_attend(c, prob, acc, True, True)
+
+
 def test_attend_longest_context(jacap):
     c = Case([131072], 1, BF, 128, H=1, G=8, seed=9)
     prob, acc = run_attend(jacap, c, False, True)
@@ -193,7 +219,7 @@ def test_rows_that_see_nothing(jacap, dtype, S):
 
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
-@pytest.mark.parametrize("S", [2, 21])
+@pytest.mark.parametrize("S", [2, 7, 11, 21, 50])
 def test_non_finite_values_in_hidden_places(jacap, dtype, d, S, value):
     """K and V of empty slots, of rows past the live lengths and of drafted tokens
     that a row does not see take no part in that row."""
