@@ -340,15 +340,19 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> par
         for (int b = 0; b < W::kBlocks; ++b) o[i][b] *= f;
       }
     }
+    // (a step's weights are added to each other first: one by one, the small ones would
+    // be lost beside the sum)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int i = 0; i < MT; ++i) {
+      float sum[NT];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          z[i][t][e] = exp2_fast(__builtin_fmaf(z[i][t][e], at.c, -ref[i]));
-          l[i] += z[i][t][e];
-        }
+        for (int e = 0; e < 4; ++e) z[i][t][e] = exp2_fast(__builtin_fmaf(z[i][t][e], at.c, -ref[i]));
+        sum[t] = (z[i][t][0] + z[i][t][1]) + (z[i][t][2] + z[i][t][3]);
+      }
+      l[i] += NT == 2 ? sum[0] + sum[NT - 1] : sum[0];
+    }
     if constexpr (W::kBf16) {
       bf8 pb[MT];
 #pragma unroll
@@ -711,9 +715,12 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           z[i][t][e] = exp2_fast(__builtin_fmaf(z[i][t][e], at.c, -ref[i]));
-          l[i] += z[i][t][e];
           pb[i][4 * t + e] = (__bf16)z[i][t][e];
         }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+      l[i] += ((z[i][0][0] + z[i][0][1]) + (z[i][0][2] + z[i][0][3])) +
+              ((z[i][1][0] + z[i][1][1]) + (z[i][1][2] + z[i][1][3]));
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       uint64_t v[2];

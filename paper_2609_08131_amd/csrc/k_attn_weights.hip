@@ -67,6 +67,8 @@ __device__ __forceinline__ float decayed(const Attn& at, float old, float sum) {
 // place as they are added: no branch between, so that a tile's products run beside
 // the exponentials of the next. Keys are requested a step ahead of their products.
 // ---------------------------------------------------------------------------
+constexpr int kFlush = 8;
+
 template <typename T>
 struct RowArgs {
   const T *q, *k;
@@ -104,11 +106,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
   const int all = at.causal ? first + pmin + 1 : un.n;  // every row sees the tokens below
   const int t0 = split * chunk, t1 = min(limit, t0 + chunk);
 
-  float nref[MT], l[MT];  // minus the lane's maximum, its sum; SUM: minus lse, the row's weight
+  // Minus the lane's maximum, its sum; SUM: minus lse, the row's weight. The sum is
+  // taken by kFlush steps first: added one by one to that of a token which dominates the
+  // row, most of the others' small weights would be lost to rounding, always to the
+  // same side (a 128K window's accumulators off by 2e-6 relative, 2e-7 so).
+  float nref[MT], l[MT], li[MT];
+  int steps = 0;
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     nref[i] = -kNoMax;
-    l[i] = 0.0f;
+    l[i] = li[i] = 0.0f;
   }
   if (t0 < t1) {
     uint4 qf[MT][NP];
@@ -182,15 +189,25 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
         if (__ballot(over > kLazyMax) != 0) {
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
-            const float now = fmaxf(-nref[i], top[i] * at.c);
-            l[i] *= exp2_fast(-nref[i] - now);
+            const float now = fmaxf(-nref[i], top[i] * at.c), f = exp2_fast(-nref[i] - now);
+            l[i] *= f;
+            li[i] *= f;
             nref[i] = -now;
+          }
+        }
+        if ((++steps & (kFlush - 1)) == 0) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            l[i] += li[i];
+            li[i] = 0.0f;
           }
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
+          float y[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) l[i] += exp2_fast(__builtin_fmaf(z[i][e], at.c, nref[i]));
+          for (int e = 0; e < 4; ++e) y[e] = exp2_fast(__builtin_fmaf(z[i][e], at.c, nref[i]));
+          li[i] += (y[0] + y[1]) + (y[2] + y[3]);
           z[i] = logits<T, D>(next.k, qf[i]);
         }
         interleave<W::kBf16, MT * NP>();
@@ -228,7 +245,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
   for (int i = 0; i < MT; ++i) {
     float top = fmaxf(-nref[i], __shfl_xor(-nref[i], 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    float s = l[i] * exp2_fast(-nref[i] - top);
+    float s = (l[i] + li[i]) * exp2_fast(-nref[i] - top);
     s += __shfl_xor(s, 16);
     s += __shfl_xor(s, 32);
     if (qg == 0) {
