@@ -339,8 +339,7 @@ jacap_status jacap_evict_weighted_slots(const jacap_config* cfg, const jacap_bat
   Launch& L = A.base;
   L.ws.kept = 256;
   TimedPhase tp(L.stream, JACAP_PHASE_SELECT);
-  JACAP_TRY(launch_select_evicted(L, acc, slots, slot_cap));
-  JACAP_TRY(launch_mark_slots(L, slots, slot_cap, acc));
+  JACAP_TRY(launch_select_empty(L, acc, slots, slot_cap));
   return JACAP_OK;
 }
 

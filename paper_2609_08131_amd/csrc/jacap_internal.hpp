@@ -468,8 +468,8 @@ hipError_t launch_compact(const Launch& L, const int32_t* idx, const void* k, co
 hipError_t launch_compact_weighted(const Launch& L, const int32_t* idx, const void* k,
                                    const void* v, void* ko, void* vo, const float* acc,
                                    float* acc_out, int64_t as, int64_t al, int64_t ah);
-// acc[slot] = -1 for the listed slots of every unit.
-hipError_t launch_mark_slots(const Launch& L, const int32_t* slots, int cap, float* acc);
+// launch_select_evicted by the accumulators, whose listed slots become empty (-1).
+hipError_t launch_select_empty(const Launch& L, float* acc, int32_t* slots, int cap);
 hipError_t launch_greedy(const Launch& L, const void* v, int32_t* idx, int32_t* order,
                          double* logdet);
 

@@ -768,22 +768,29 @@ hipError_t launch_select(const Launch& L, const float* scores, int32_t* idx) {
 // threads write consecutive slots between kept positions). The tile also
 // writes the -1 padding of the slots [p0, p0 + kEvTile) at or past n - kept,
 // and the last tile every padding slot beyond. Units whose list select_kernel has
-// written already are skipped.
+// written already are skipped. mark != null: the accumulators [L][H][T], of which the
+// evicted positions' entries become -1 (empty slots).
 // ---------------------------------------------------------------------------
 constexpr int kEvTile = 4096;
 
 template <class C>
 __global__ __launch_bounds__(kThreads) void evicted_kernel(Geo g, const int32_t* __restrict__ kept,
                                                            int budget, int protect,
-                                                           int32_t* __restrict__ slots, int cap) {
+                                                           int32_t* __restrict__ slots, int cap,
+                                                           float* __restrict__ mark) {
   const int u = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x;
   const Unit un = live_unit(g, u);
   const int n = un.n, kk = min(budget, n), ne = n - kk;
   const int npro = min(protect, kk);
-  if (ranks_evicted<C>(n - npro, kk - npro)) return;
   const int32_t* kp = kept + (int64_t)u * budget;
   int32_t* out = slots + (int64_t)u * cap;
   const int p0 = tile * kEvTile;
+  float* gone = mark ? mark + token_row(g, un) : nullptr;
+  if (ranks_evicted<C>(n - npro, kk - npro)) {
+    if (gone)
+      for (int j = p0 + tid; j < min(ne, p0 + kEvTile); j += kThreads) gone[out[j]] = -1.0f;
+    return;
+  }
   const int pad_hi = tile == (int)gridDim.x - 1 ? cap : min(cap, p0 + kEvTile);
   for (int j = max(ne, p0) + tid; j < pad_hi; j += kThreads) out[j] = -1;
   if (p0 >= n) return;
@@ -799,10 +806,12 @@ __global__ __launch_bounds__(kThreads) void evicted_kernel(Geo g, const int32_t*
     const int r = lower_bound_lds(ks, cnt, i);
     if (r < cnt && ks[r] == i) continue;  // kept
     out[i - (lo + r)] = i;                // i - (lo + r) < ne for an evicted i
+    if (gone) gone[i] = -1.0f;
   }
 }
 
-hipError_t launch_select_evicted(const Launch& L, const float* scores, int32_t* slots, int cap) {
+static hipError_t evicted_launch(const Launch& L, const float* scores, int32_t* slots, int cap,
+                                 float* mark) {
   const int budget = L.cfg->budget_k;
   int32_t* kept = ws_ptr<int32_t>(L.wsp, L.ws.kept);
   if (budget > 0) {
@@ -812,11 +821,19 @@ hipError_t launch_select_evicted(const Launch& L, const float* scores, int32_t* 
   const int tiles = std::max(1, (L.geo.maxn + kEvTile - 1) / kEvTile);
   auto go = [&](auto kern) {
     kern<<<dim3(tiles, L.geo.U), kThreads, 0, L.stream>>>(L.geo, kept, budget, L.cfg->protect_last,
-                                                          slots, cap);
+                                                          slots, cap, mark);
   };
   if (select_narrow(L)) go(evicted_kernel<SelNarrow>);
   else go(evicted_kernel<SelWide>);
   return hipGetLastError();
+}
+
+hipError_t launch_select_evicted(const Launch& L, const float* scores, int32_t* slots, int cap) {
+  return evicted_launch(L, scores, slots, cap, nullptr);
+}
+
+hipError_t launch_select_empty(const Launch& L, float* acc, int32_t* slots, int cap) {
+  return evicted_launch(L, acc, slots, cap, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -943,25 +960,6 @@ hipError_t launch_compact_weighted(const Launch& L, const int32_t* idx, const vo
                                    const void* v, void* ko, void* vo, const float* acc,
                                    float* acc_out, int64_t as, int64_t al, int64_t ah) {
   return compact_launch<true>(L, idx, k, v, ko, vo, Weighted{acc, acc_out, as, al, ah});
-}
-
-// Empty slots of a cache refilled in place: the listed positions (-1: none) of
-// each unit, whose lists the selection has written before.
-__global__ __launch_bounds__(kThreads) void mark_slots_kernel(Geo g,
-                                                              const int32_t* __restrict__ slots,
-                                                              int cap, float* __restrict__ acc) {
-  const int u = blockIdx.y, j = blockIdx.x * kThreads + threadIdx.x;
-  if (j >= cap) return;
-  const Unit un = live_unit(g, u);
-  const int t = slots[(int64_t)u * cap + j];
-  if (t >= 0 && t < un.n) acc[token_row(g, un) + t] = -1.0f;
-}
-
-hipError_t launch_mark_slots(const Launch& L, const int32_t* slots, int cap, float* acc) {
-  if (cap == 0) return hipSuccess;
-  mark_slots_kernel<<<dim3((cap + kThreads - 1) / kThreads, L.geo.U), kThreads, 0, L.stream>>>(
-      L.geo, slots, cap, acc);
-  return hipGetLastError();
 }
 
 }  // namespace jacap
