@@ -25,6 +25,7 @@ constexpr int kKeepRows = 16;
 constexpr int kSpans = 512;           // workgroups the attention of few rows is cut into, of
 constexpr int kSpanMin = 256;         // ... at least this many tokens
 constexpr int kUnitGroups = 4;        // what beginning and ending a unit costs, in groups of 4 steps
+constexpr int64_t kMaxGroups = INT32_MAX / 2;  // groups of a batch
 constexpr int kWideChunkMin = 256;    // tokens per workgroup of many rows, at least
 constexpr int kWideRows = 32;         // more rows than these share K and V through LDS (bf16),
 constexpr int kWideBlocks = 256;      // a workgroup per compute unit

@@ -175,7 +175,7 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   const int64_t groups =
       (int64_t)g.L * g.H * w->row_blocks * (g.T / 64 + (int64_t)g.B * (1 + kUnitGroups));
   if (((int64_t)g.U * w->splits + 8) * w->row_blocks > kMaxGrid || UR + g.U * token_blocks > kMaxGrid ||
-      groups > INT32_MAX / 2 || pieces > INT32_MAX || !sum_grid_ok(g, *sum))
+      groups > kMaxGroups || pieces > INT32_MAX || !sum_grid_ok(g, *sum))
     return JACAP_ERR_UNSUPPORTED;
   return JACAP_OK;
 }

@@ -130,10 +130,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> par
   auto groups64 = [&](const int2& x) { return x.y < 0 ? 0 : real_groups(x.y, GROUP) + kUnitGroups; };
   int2 held = rows64(0);
   int held_b = 0;
-  int seq_groups = 0;
+  int64_t seq_groups = 0;
   for (int b0 = 0; b0 < B; b0 += 64)
-    seq_groups += __builtin_amdgcn_readlane(wave_scan(groups64(b0 == 0 ? held : rows64(b0))), 63);
-  const int total = seq_groups * per_seq;
+    seq_groups += (uint32_t)__builtin_amdgcn_readlane(wave_scan(groups64(b0 == 0 ? held : rows64(b0))), 63);
+  // (more than the host allowed for: offsets that go back and forth, flagged; no work)
+  const int total = seq_groups * per_seq <= kMaxGroups ? (int)(seq_groups * per_seq) : 0;
   const int quantum = span_quantum(total, gridDim.x, GROUP);
   int at_group = blockIdx.x * quantum;
   const int end_group = min(total, at_group + quantum);
@@ -527,7 +528,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> par
       int sum = 0;
       for (int b0 = 0; b0 < B; b0 += 64) {
         const int incl = sum + wave_scan(groups64(rows64(b0)));
-        if (b0 + lane < B) params.p.before[b0 + lane + 1] = incl;
+        if (b0 + lane < B) params.p.before[b0 + lane + 1] = total > 0 ? incl : 0;
         sum = __builtin_amdgcn_readlane(incl, 63);
       }
       if (lane == 0) params.p.before[0] = 0;

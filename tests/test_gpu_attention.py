@@ -392,6 +392,22 @@ def test_bad_lengths_are_flagged_and_taken_as_empty(jacap):
         check_attend(c, prob, None, False, False)
 
 
+@pytest.mark.parametrize("S", [1, 40])
+def test_inconsistent_offsets(jacap, S):
+    """Offsets that go back, or past the rows: flagged, the sequence taken as empty."""
+    for offs in ([0, 40, 10, 50], [0, 40, 90, 200], [0, 40, -3, 5]):
+        c = Case([40, 0, 0], S, BF, 64, seed=3)
+        big = Case([40, 50, 0], S, BF, 64, seed=3)
+        c.k, c.v, c.acc = big.k, big.v, big.acc
+        c.offsets = torch.tensor(offs, dtype=torch.int32, device="cuda")
+        p = jacap.AttentionParams()
+        prob = jacap.prepare_attend(c.q, c.k, c.v, c.kd, c.vd, c.offsets, [40, 40, 10], p)
+        jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd)
+        assert jacap.read_status(prob.ws) == jacap.FLAG_BAD_OFFSETS
+        c.lens = [40]
+        check_attend(c, prob, None, False, False)
+
+
 def test_deterministic(jacap):
     c = Case([9000, 77, 1300], 9, BF, 128, tree="tree", seed=3)
     a, acc_a = run_attend(jacap, c, False, True)
