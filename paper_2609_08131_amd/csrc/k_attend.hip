@@ -984,7 +984,8 @@ __device__ __forceinline__ Pieces pieces_of(const Geo& g, const JoinGeo& j, cons
   return {(start + c - 1) / q - start / q + 1, start, q, j.rows, r % j.rows};
 }
 
-template <typename T, int D>
+// ROWS: at least the rows whose logits are kept.
+template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, JoinArgs<T> p,
                                                                JoinGeo jg, int few, int rows_grid,
                                                                int token_blocks) {
@@ -1056,7 +1057,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   const float* z = p.z + keep_at(g, un, R, t0 / 16 + tid / 16) + tid % 16;
   const int left = un.n - t0;
   constexpr int PER = kJoinTokens / kThreads;
-  float old[PER], sum[PER], y[kKeepRows][PER];
+  float old[PER], sum[PER], y[ROWS][PER];
   auto logit = [&](int r, int x) {
     return tid + x * kThreads < left ? z[x * (kThreads / 16) * R * 16 + r * 16] : -INFINITY;
   };
@@ -1065,7 +1066,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     old[x] = tid + x * kThreads < left ? p.acc[tr + tid + x * kThreads] : -1.0f;
     sum[x] = 0.0f;
 #pragma unroll
-    for (int r = 0; r < kKeepRows; ++r)
+    for (int r = 0; r < ROWS; ++r)
       if (r < R) y[r][x] = logit(r, x);
   }
   __shared__ float slse[kKeepRows], sw[kKeepRows];
@@ -1110,7 +1111,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
       for (int x = 0; x < PER; ++x) sum[x] = __builtin_fmaf(w, exp2_fast(v[x] - ls), sum[x]);
   };
 #pragma unroll
-  for (int r = 0; r < kKeepRows; ++r)
+  for (int r = 0; r < ROWS; ++r)
     if (r < R) add(r, y[r]);
 #pragma unroll
   for (int x = 0; x < PER; ++x)
@@ -1144,8 +1145,11 @@ static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, void* ou
   const int rows_grid = wide && w.splits == 1 ? 0 : (int)((UR + per - 1) / per);
   const int token_blocks = std::max(1, (g.maxn + kJoinTokens - 1) / kJoinTokens);
   const int64_t grid = rows_grid + (w.keep ? (int64_t)g.U * token_blocks : 0);
-  attend_join_kernel<T, D><<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, jg, few, rows_grid,
-                                                                           token_blocks);
+  auto go = [&](auto kern) {
+    kern<<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, jg, few, rows_grid, token_blocks);
+  };
+  if (!w.keep || A.at.R <= 4) go(attend_join_kernel<T, D, 4>);
+  else go(attend_join_kernel<T, D, kKeepRows>);
   return hipGetLastError();
 }
 
