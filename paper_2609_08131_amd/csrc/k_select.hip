@@ -22,7 +22,7 @@
 // The pass checks that the bounds hold (fewer than budget tokens above hi, at
 // least budget at or above lo) and that the lists fit; otherwise the unit takes
 // the general path: a three-pass radix select over the scores (11 + 11 + 10
-// bits, MSB first) and an ordered emission pass, several times slower. All paths
+// bits, MSB first) and an ordered emission pass, two to three times slower. All paths
 // give the same, deterministic result.
 //
 // The first two count with wave ballots: a wave takes 64 consecutive positions per
@@ -291,8 +291,10 @@ __device__ __forceinline__ uint32_t block_exclusive_scan(uint32_t x, uint32_t* s
 
 // Radix select (11 + 11 + 10 bits, MSB first): the key of rank `rank`
 // (1 = largest, rank <= cnt) among key_at(0 .. cnt-1); `need` = how many keys
-// equal to it fall within the top `rank`.
-template <class C, class KeyAt>
+// equal to it fall within the top `rank`. TIES: eight keys a thread are loaded
+// at a time, and those of a wave that share its first active lane's digit are counted by
+// one atomic (where most keys are equal, as empty slots are, their one bin is the whole time).
+template <class C, bool TIES = false, class KeyAt>
 __device__ __forceinline__ uint32_t radix_rank(KeyAt key_at, int cnt, uint32_t rank,
                                                SelShared<C>& sh, uint32_t& need) {
   const int tid = threadIdx.x;
@@ -306,9 +308,26 @@ __device__ __forceinline__ uint32_t radix_rank(KeyAt key_at, int cnt, uint32_t r
     for (uint32_t i = tid; i < nb; i += C::kThreads) sh.hist[i] = 0u;
     if (tid == 0) { sh.bc[0] = 0u; sh.bc[1] = 0u; }
     __syncthreads();
-    for (int i = tid; i < cnt; i += C::kThreads) {
-      const uint32_t key = key_at(i);
-      if ((key & pmask) == prefix) atomicAdd(&sh.hist[(key >> shf) & dmask], 1u);
+    if constexpr (TIES) {
+      for (int i0 = tid; i0 < cnt; i0 += 8 * C::kThreads) {
+        uint32_t key[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) key[j] = key_at(min(i0 + j * C::kThreads, cnt - 1));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (i0 + j * C::kThreads >= cnt || (key[j] & pmask) != prefix) continue;
+          const uint32_t digit = (key[j] >> shf) & dmask;
+          const uint32_t first = __builtin_amdgcn_readfirstlane(digit);
+          const uint64_t same = __ballot(digit == first);
+          if (digit != first) atomicAdd(&sh.hist[digit], 1u);
+          else if ((tid & 63) == __builtin_ctzll(same)) atomicAdd(&sh.hist[first], (uint32_t)__popcll(same));
+        }
+      }
+    } else {
+      for (int i = tid; i < cnt; i += C::kThreads) {
+        const uint32_t key = key_at(i);
+        if ((key & pmask) == prefix) atomicAdd(&sh.hist[(key >> shf) & dmask], 1u);
+      }
     }
     __syncthreads();
     // Suffix counts from the top digit down: each thread owns a contiguous run
@@ -337,37 +356,54 @@ __device__ __forceinline__ uint32_t radix_rank(KeyAt key_at, int cnt, uint32_t r
   return prefix;
 }
 
-// General path: radix select over the scores, then an ordered emission pass
-// over contiguous per-thread segments.
+// General path: radix select over the scores, then an ordered emission pass by ballots
+// (20 units of 93567 tokens of which all but 346 are empty slots, keeping 349, with the
+// path before it: 370 us with one atomic per key and a contiguous segment per thread, 134
+// now).
 template <class C, int DIR>
 __device__ __forceinline__ void select_general(const RankedScores<DIR>& rs, int kk,
                                                const SelOut<DIR>& out, SelShared<C>& sh) {
-  const int tid = threadIdx.x, n = rs.n;
-  auto key_at = [&](int i) { return rs.key(i); };
+  const int lane = threadIdx.x & 63, n = rs.n;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int par = 0;
   uint32_t need;
-  const uint32_t T = radix_rank<C>(key_at, n, (uint32_t)kk, sh, need);
-  const int seg = (n + C::kThreads - 1) / C::kThreads;
-  const int lo = min(n, tid * seg), hi = min(n, lo + seg);
-  uint32_t cgt = 0, ceq = 0;
-  for (int i = lo; i < hi; ++i) {
-    const uint32_t key = key_at(i);
-    cgt += key > T;
-    ceq += key == T;
-  }
-  uint32_t tot;
-  uint32_t gt_before = block_exclusive_scan<C>(cgt, sh.scan, tot);
-  uint32_t eq_before = block_exclusive_scan<C>(ceq, sh.scan, tot);
-  for (int i = lo; i < hi; ++i) {
-    const uint32_t key = key_at(i);
-    if (key > T) {
-      const uint32_t pos = gt_before + min(eq_before, need);
-      if (pos < (uint32_t)kk) out.put((int)pos, i);
-      ++gt_before;
-    } else if (key == T) {
-      const uint32_t pos = gt_before + eq_before;
-      if (eq_before < need && pos < (uint32_t)kk) out.put((int)pos, i);
-      ++eq_before;
+  const uint32_t T = radix_rank<C, true>([&](int i) { return rs.key(i); }, n, (uint32_t)kk, sh, need);
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  float nxt[C::kPer];
+  auto pos = [&](int base, int j) { return base + (wave * C::kPer + j) * 64 + lane; };
+  auto load_chunk = [&](int base) {
+#pragma unroll
+    for (int j = 0; j < C::kPer; ++j) nxt[j] = rs.raw(min(pos(base, j), n - 1));
+  };
+  load_chunk(0);
+  uint32_t gt = 0, eq = 0;  // keys > T and == T so far
+  for (int base = 0; base < n; base += C::kChunk) {
+    uint32_t k[C::kPer];
+#pragma unroll
+    for (int j = 0; j < C::kPer; ++j) k[j] = rs.conv(nxt[j]);
+    if (base + C::kChunk < n) load_chunk(base + C::kChunk);  // uniform
+    uint64_t mg[C::kPer], me[C::kPer];
+    uint32_t ng = 0, ne = 0;
+#pragma unroll
+    for (int j = 0; j < C::kPer; ++j) {
+      mg[j] = __ballot(pos(base, j) < n && k[j] > T);
+      me[j] = __ballot(pos(base, j) < n && k[j] == T);
+      ng += __popcll(mg[j]);
+      ne += __popcll(me[j]);
     }
+    uint2 before;
+    const uint2 tot = wave_exchange<C>(make_uint2(ng, ne), sh, par, before);
+    uint32_t g0 = gt + before.x, e0 = eq + before.y;
+#pragma unroll
+    for (int j = 0; j < C::kPer; ++j) {
+      const uint32_t e = e0 + __popcll(me[j] & below);
+      if ((mg[j] >> lane & 1) || ((me[j] >> lane & 1) && e < need))
+        out.put((int)(g0 + __popcll(mg[j] & below) + min(e, need)), pos(base, j));
+      g0 += __popcll(mg[j]);
+      e0 += __popcll(me[j]);
+    }
+    gt += tot.x;
+    eq += tot.y;
   }
 }
 
@@ -457,36 +493,44 @@ __device__ __forceinline__ bool select_sampled(const RankedScores<DIR>& rs, int 
 #pragma unroll
     for (int j = 0; j < C::kPer; ++j) nxt[j] = rs.raw(min(pos(base, j), n - 1));
   };
-  load_chunk(0);
   uint32_t ccnt = 0;
-  for (int base = 0; base < n; base += C::kChunk) {
-    uint32_t k[C::kPer];
+  // A second pass from lo + 1: where most keys are equal (empty slots), lo is that key,
+  // and the keys above it are few (20 units of 93567 tokens, 560 of them not empty: 245 us
+  // where the general path takes over, 57 so). The first ends as soon as its list is full.
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    load_chunk(0);
+    ccnt = 0;
+    for (int base = 0; base < n && ccnt <= (uint32_t)C::kCand; base += C::kChunk) {
+      uint32_t k[C::kPer];
 #pragma unroll
-    for (int j = 0; j < C::kPer; ++j) k[j] = rs.conv(nxt[j]);
-    if (base + C::kChunk < n) load_chunk(base + C::kChunk);  // uniform
-    uint64_t cand[C::kPer];
-    uint32_t nc = 0;
+      for (int j = 0; j < C::kPer; ++j) k[j] = rs.conv(nxt[j]);
+      if (base + C::kChunk < n) load_chunk(base + C::kChunk);  // uniform
+      uint64_t cand[C::kPer];
+      uint32_t nc = 0;
 #pragma unroll
-    for (int j = 0; j < C::kPer; ++j) {
-      cand[j] = __ballot(pos(base, j) < n && k[j] >= lo);
-      nc += __popcll(cand[j]);
-    }
-    uint2 before;
-    const uint2 tot = wave_exchange<C>(make_uint2(nc, 0u), sh, par, before);
-    uint32_t co = ccnt + before.x;
-#pragma unroll
-    for (int j = 0; j < C::kPer; ++j) {
-      const uint32_t at = co + __popcll(cand[j] & below);
-      if ((cand[j] >> lane & 1) && at < (uint32_t)C::kCand) {
-        sh.ckey[at] = k[j];
-        sh.cpos[at] = pos(base, j);
+      for (int j = 0; j < C::kPer; ++j) {
+        cand[j] = __ballot(pos(base, j) < n && k[j] >= lo);
+        nc += __popcll(cand[j]);
       }
-      co += __popcll(cand[j]);
+      uint2 before;
+      const uint2 tot = wave_exchange<C>(make_uint2(nc, 0u), sh, par, before);
+      uint32_t co = ccnt + before.x;
+#pragma unroll
+      for (int j = 0; j < C::kPer; ++j) {
+        const uint32_t at = co + __popcll(cand[j] & below);
+        if ((cand[j] >> lane & 1) && at < (uint32_t)C::kCand) {
+          sh.ckey[at] = k[j];
+          sh.cpos[at] = pos(base, j);
+        }
+        co += __popcll(cand[j]);
+      }
+      ccnt += tot.x;
     }
-    ccnt += tot.x;
+    if (ccnt <= (uint32_t)C::kCand) break;  // uniform: the same count in every thread
+    ++lo;
   }
   __syncthreads();
-  // uniform: the same count in every thread
   if (ccnt < (uint32_t)kk || ccnt > (uint32_t)C::kCand) return false;
   // T among the candidates; fewer keys per thread cost less.
   if (ccnt <= (uint32_t)C::kThreads) keep_candidates<C, 1>(ccnt, (uint32_t)kk, out, sh, par);

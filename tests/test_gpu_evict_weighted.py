@@ -234,3 +234,30 @@ def test_decoding_loop(jacap, dtype):
                     ck[0, h, b * cap + s] = kd[b, 0, h, node]
                     cv[0, h, b * cap + s] = vd[b, 0, h, node]
                     cacc[0, h, b * cap + s] = 0.0
+
+
+@pytest.mark.parametrize("units,n,budget,live", [
+    (2, 40000, 300, 0), (2, 40000, 300, 290), (2, 40000, 300, 300), (2, 40000, 300, 310),
+    (2, 40000, 300, 9000), (2, 40000, 12000, 11000), (2, 33000, 32000, 20000),
+    (1024, 9001, 700, 650), (1024, 9001, 300, 290), (1024, 9001, 300, 310)])
+def test_slots_of_mostly_empty_caches(jacap, units, n, budget, live):
+    """Units of which all but `live` tokens are empty slots already: fewer than the
+    budget, as many, and more; in both launch shapes."""
+    gen = torch.Generator().manual_seed(n + budget + live)
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    k = torch.zeros((units, 1, n, 64), dtype=torch.bfloat16, device="cuda")
+    p = jacap.prepare_evict_weighted(k, k, off, [n], budget=budget)
+    acc = torch.full((units, 1, n), -1.0)
+    for u in range(units):
+        # values of 50 steps: many equal ones at the threshold
+        acc[u, 0, torch.randperm(n, generator=gen)[:live]] = (
+            torch.randint(0, 50, (live,), generator=gen).float())
+    order = torch.argsort(-acc.double(), dim=-1, stable=True)
+    want = acc.clone()
+    want.scatter_(-1, order[..., budget:], -1.0)
+    gone = torch.sort(order[..., budget:], dim=-1).values
+    dev = acc.cuda()
+    slots = torch.empty((1, units, 1, n - budget), dtype=torch.int32, device="cuda")
+    jacap.run_evict_weighted_slots(p, dev, slots)
+    assert torch.equal(dev.cpu(), want)
+    assert torch.equal(slots.cpu()[0].long(), gone)
