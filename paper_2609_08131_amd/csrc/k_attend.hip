@@ -1052,7 +1052,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   const Unit un = live_unit(g, u);
   const int t0 = blk * kJoinTokens;
   if (t0 >= un.n && blk > 0) return;
-  // The entries and the rows' logits are requested before the rows' lse is joined. Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
+  // The entries and the rows' logits are requested before the rows' lse is joined.
+  // Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
   const int64_t tr = token_row(g, un) + t0;
   const float* z = p.z + keep_at(g, un, R, t0 / 16 + tid / 16) + tid % 16;
   const int left = un.n - t0;
