@@ -76,36 +76,39 @@ jacap_status check_attend(const jacap_config* cfg, const jacap_batch* batch,
   return JACAP_OK;
 }
 
-// Tokens per workgroup: halved from `most` to `least` while the batch's chunks
-// times `per` stay below `blocks` workgroups.
-int chunk_tokens(const Geo& g, int64_t per, int most, int least, int blocks) {
-  const int64_t LHT = (int64_t)g.L * g.H * g.T;
-  int chunk = most;
-  while (chunk > least && LHT / chunk * per < blocks) chunk /= 2;
-  return chunk;
-}
-
 // How the passes over rows and tokens of the weights are cut; `o` the
-// workspace's size so far. The sums of few rows stream the keys past the rows,
-// as the log-sums do; those of more hold keys and stream rows (log-sums and sums of 4
-// rows, 131072 tokens, 8 heads: 89 us streaming keys, 121 holding them; of 128 rows,
-// 8192 tokens: 27 and 26; of 256 rows, 4 layers of 131072: 970 and 875).
+// workspace's size so far. The chunks of the passes with rows in registers are one round
+// of the chip (fp32 rows, 32768 tokens: 92 us, 102 with chunks of half the size; five
+// sequences of 100 to 30000 tokens 120 and 141, equal long ones the same). The sums of
+// few rows stream the keys past the rows, as the log-sums do (log-sums and sums of 4
+// rows, 131072 tokens, 8 heads: 89 us streaming keys, 121 holding them); more rows
+// stay in LDS, a stretch of tokens passing them (256 rows, 4 layers of 131072 tokens:
+// 718 us with the log-sums, 865 with the rows staged for every 256 tokens; 100 rows,
+// 2 layers of 65536: 111 and 141; 256 rows of 1000 tokens 26.7 and 25.6, from the split
+// of their rows); and more than fit there are staged, in parts while the grid is small.
 void layout_sum(const Geo& g, const Attn& at, bool bf16, WeightsSpace* w, size_t* o) {
   const int64_t LHT = (int64_t)g.L * g.H * g.T;
   const int tiles = (at.R + 15) / 16;
   w->mt = !bf16 ? kRowTilesFp32 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : kRowTilesBf16;
   w->row_blocks = (tiles + w->mt - 1) / w->mt;
-  w->chunk = chunk_tokens(g, w->row_blocks, kRowsChunk, kRowsChunkMin, kWeightsBlocks);
+  const int64_t per_block = (LHT * w->row_blocks / kRowsBlocks + 63) / 64 * 64;
+  w->chunk = (int)std::max<int64_t>(kRowsChunkMin, std::min<int64_t>(per_block, kRowsChunk));
   w->chunks = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
   w->tiles = bf16 ? kSumTilesBf16 : kSumTilesFp32;
   const int tokens = 64 * w->tiles;
   w->blocks = (g.maxn + tokens - 1) / tokens;
   w->stream_keys = tiles <= (bf16 ? kStreamTilesBf16 : kStreamTilesFp32);
-  const int64_t grid = std::max<int64_t>(1, LHT / tokens);
-  w->row_splits = w->stream_keys
-                      ? 1
-                      : (int)std::max<int64_t>(1, std::min<int64_t>(kWeightsBlocks / grid,
-                                                                    at.R / kSumRowsMin));
+  w->held = 0;
+  w->row_splits = 1;
+  if (!w->stream_keys && at.R <= held_rows(g.D * (bf16 ? 2 : 4))) {
+    const int64_t per = (LHT / kHeldBlocks + tokens - 1) / tokens * tokens;
+    w->held = (int)std::min<int64_t>(std::max<int64_t>(per, tokens), 1 << 20);
+    w->blocks = (g.maxn + w->held - 1) / w->held;
+  } else if (!w->stream_keys) {
+    const int64_t grid = std::max<int64_t>(1, LHT / tokens);
+    w->row_splits =
+        (int)std::max<int64_t>(1, std::min<int64_t>(kSumBlocks / grid, at.R / kSumRowsMin));
+  }
   w->part = *o;
   if (w->row_splits > 1) *o = align256(*o + 4 * (size_t)w->row_splits * LHT);
 }

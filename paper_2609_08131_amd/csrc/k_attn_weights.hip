@@ -7,7 +7,7 @@
 // A token's sum needs every row's lse first, and a row's lse every token, so
 // the logits are formed twice: a pass over the rows' blocks for lse (rows in
 // registers, keys streamed), and a pass over the tokens' blocks for the sums
-// (keys in registers, rows streamed). Neither writes logits. V is not read.
+// (keys in registers, rows from LDS). Neither writes logits. V is not read.
 #include <algorithm>
 
 #include "attention.hpp"
@@ -565,6 +565,143 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_kernel(Geo g, Attn at, S
   if (blockIdx.x == 0 && p.status) write_status(g, p.status);
 }
 
+// ---------------------------------------------------------------------------
+// Sums from the few rows of a window or a tree: all of a unit's rows lie in LDS for the whole of a workgroup's stretch of tokens. A wave takes its
+// stretch's blocks of 16 NT tokens in turn (their keys in registers, the next block's
+// requested during the last row tile) past the rows, with no barrier after the first.
+// z is carried over the blocks' ends too: a block's last logits are added, and its
+// accumulators written, as the next one's first are formed. A tile of 16 x 16 logits
+// is 96 cycles of vector instructions (an FMA, an exponential at a quarter of the rate
+// and an FMA per logit) and 64 of MFMA at d = 128. 256 rows, 32 units of 131072 tokens: 326
+// us, 430 over calls without a pause, as the clock falls; a large library product of as many
+// operations takes 240, and with the rows staged for every 256 tokens it was 530 to 590.
+// ---------------------------------------------------------------------------
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(kThreads, 2) void attn_sum_held_kernel(Geo g, Attn at, SumArgs<T> p,
+                                                                   int chunk) {
+  using W = Row<T, D>;
+  constexpr int NP = W::kPieces, WAVES = kThreads / 64;
+  constexpr int STAGE = W::kBf16 ? 4 : 2;  // row tiles unrolled
+  constexpr int ROWS = held_rows(W::kBytes);
+  constexpr int STEP = 16 * NT * WAVES;
+  const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int u = blockIdx.x % g.U;
+  const Unit un = live_unit(g, u);
+  const int begin = blockIdx.x / g.U * chunk, end = begin + min(chunk, un.n - begin);
+  const int R = at.R, w = g.w;
+  const int first = un.n - w;  // position of row 0 (causal)
+  __shared__ __align__(16) uint4 rows_lds[ROWS / 16][NP][64];  // as the MFMA takes them
+  struct Meta { float lse, weight; };
+  __shared__ Meta meta[ROWS];
+  __shared__ int last_lds[ROWS];  // last position seen, -1: adds nothing
+
+  if (begin < end) {
+    const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
+    const int32_t ks = (int32_t)(g.kst * sizeof(T));
+    float* accu = p.acc + token_row(g, un);
+    uint4 kf[NT][NP];
+    float old[NT];
+    int tok = begin + wave * 16 * NT;
+    auto fetch = [&](int t, int b) {  // tile t of the block at b (zeros past the stretch's end)
+      const int r0 = b + 16 * t;
+      const auto kr = buffer_range(kb + r0 * g.kst, rows_bytes(min(16, end - r0), ks, W::kBytes));
+#pragma unroll
+      for (int a = 0; a < NP; ++a) kf[t][a] = buffer_load16(kr, m * ks + 64 * a + 16 * qg);
+    };
+#pragma unroll
+    for (int t = 0; t < NT; ++t) fetch(t, tok);
+
+    const T* qu = unit_queries(g, un, p.q);
+    const float* lseu = p.lse + ((int64_t)un.b * g.L + un.l) * g.Hq * w + (int64_t)un.h * R;
+    const float* rwu = at.row_weight ? at.row_weight + (int64_t)un.b * w : nullptr;
+    const int stages = (R + 16 * STAGE - 1) / (16 * STAGE);
+    for (int h = wave; h < STAGE * stages; h += WAVES) {
+      const int row = min(16 * h + m, R - 1), pos = row % w;
+      const float lse = lseu[row], weight = rwu ? rwu[pos] : 1.0f;
+      // (rows past the last are its copies, and add nothing)
+      const bool live = 16 * h + m < R && weight != 0.0f && lse != -INFINITY;
+      uint4 qf[NP];
+      load_row<T, D>(g, qu, row, live, qg, qf);
+#pragma unroll
+      for (int a = 0; a < NP; ++a) rows_lds[h][a][lane] = qf[a];
+      if (qg == 0) {
+        meta[16 * h + m] = Meta{live ? lse * kLog2e : 0.0f, live ? weight : 0.0f};
+        last_lds[16 * h + m] = !live ? -1 : at.causal ? first + pos : INT32_MAX;
+      }
+    }
+    __syncthreads();
+
+    f32x4 sum[NT], z[NT];
+    float ls = 0.0f, weight = 0.0f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum[t] = z[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](int t) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sum[t][e] = __builtin_fmaf(exp2_fast(__builtin_fmaf(z[t][e], at.c, -ls)), weight, sum[t][e]);
+    };
+    // the accumulators of the block at b
+    auto entries = [&](int b) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) old[t] = accu[min(b + 16 * t + 4 * qg + (m & 3), end - 1)];
+    };
+    auto write = [&](int t, int b) {
+      const float mine = tile_sum(sum[t], m);
+      const int j = b + 16 * t + 4 * qg + m;
+      if (m < 4 && j < end && !(old[t] < 0.0f)) accu[j] = decayed(at, old[t], mine);
+      sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    int before = -1;  // the block whose last logits z holds
+    for (; tok < end; tok += STEP) {
+      const bool masked = at.causal && tok + 16 * NT > first + 1;
+      for (int s = 0; s < stages; ++s) {
+#pragma unroll
+        for (int x = 0; x < STAGE; ++x) {
+          const int h = s * STAGE + x;
+          uint4 qf[NP];
+#pragma unroll
+          for (int a = 0; a < NP; ++a) qf[a] = rows_lds[h][a][lane];
+          const Meta me = meta[16 * h + m];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            add(t);
+            z[t] = logits<T, D>(kf[t], qf);
+          }
+          if (x == 0 && s == 0) {
+            if (before >= 0) {
+#pragma unroll
+              for (int t = 0; t < NT; ++t) write(t, before);
+            }
+            entries(tok);
+            before = tok;
+          }
+          if (masked) {
+            const int last = last_lds[16 * h + m];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                z[t][e] = tok + 16 * t + 4 * qg + e <= last ? z[t][e] : -INFINITY;
+          }
+          ls = me.lse;
+          weight = me.weight;
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) fetch(t, tok + STEP);
+    }
+    if (before >= 0) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        add(t);
+        write(t, before);
+      }
+    }
+  }
+  if (blockIdx.x == 0 && p.status) write_status(g, p.status);
+}
+
 // The row parts' sums, in order.
 __global__ __launch_bounds__(kThreads) void attn_sum_join_kernel(Geo g, Attn at, const float* part,
                                                                  float* acc, int row_splits) {
@@ -588,6 +725,11 @@ static hipError_t sum_typed(const AttnLaunch& A, const WeightsSpace& w, const vo
   if (w.stream_keys) {
     e = rows_tiles<T, D, true>(A, w, RowArgs<T>{(const T*)q, (const T*)k, acc, lse, nullptr, nullptr,
                                                 status});
+  } else if (w.held) {
+    attn_sum_held_kernel<T, D, NT>
+        <<<(unsigned)((int64_t)g.U * std::max(1, w.blocks)), kThreads, 0, A.base.stream>>>(
+            g, A.at, SumArgs<T>{(const T*)q, (const T*)k, lse, acc, nullptr, status}, w.held);
+    e = hipGetLastError();
   } else {
     SumArgs<T> p{(const T*)q, (const T*)k, lse, acc, part, status};
     attn_sum_kernel<T, D, NT, false>

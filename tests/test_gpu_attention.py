@@ -341,6 +341,15 @@ def test_attn_weights_long(jacap, dtype, w, lens, G):
     check_weights(jacap, c, True, decay=0.0)
 
 
+@pytest.mark.parametrize("dtype,d,w,G,causal", [
+    (BF, 128, 64, 4, True), (BF, 128, 33, 3, False), (BF, 64, 256, 1, True), (BF, 64, 13, 5, True),
+    (F32, 128, 32, 4, True), (F32, 64, 64, 4, True), (F32, 64, 11, 3, False)])
+def test_attn_weights_in_long_stretches(jacap, dtype, d, w, G, causal):
+    """Stretches of several blocks per workgroup, the last ones of each sequence cut short."""
+    c = Case([40003, 0, 3, 30001, 257], w, dtype, d, H=2, G=G, L=2, holes=0.05, spare=2, seed=21)
+    check_weights(jacap, c, causal, decay=0.75)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("causal", [False, True])
 def test_attn_weights_of_accepted_rows(jacap, dtype, causal):
