@@ -32,12 +32,10 @@ constexpr int kWideBlocks = 256;      // a workgroup per compute unit
 constexpr int kJoinFew = 16;           // pieces of a row that one group of threads joins in turn
 constexpr int kJoinRows = 1024;        // rows of a batch up to which a workgroup joins one
 constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
-// The passes with rows in registers: 16-row tiles per workgroup, at most, tokens,
+// The log-sums, rows in registers: 16-row tiles per workgroup, at most, tokens,
 // and workgroups (two per compute unit).
 constexpr int kRowTilesBf16 = 8, kRowTilesFp32 = 2;
 constexpr int kRowsChunk = 16384, kRowsChunkMin = 256, kRowsBlocks = 512;
-// 16-row tiles per KV head up to which the sums stream the keys past the rows too.
-constexpr int kStreamTilesBf16 = 4, kStreamTilesFp32 = 2;
 // The accumulation: 16-token tiles per wave (their keys in registers). The rows of a
 // unit, up to 64 KiB of them, stay in LDS for one of kHeldBlocks stretches of the tokens;
 // more are staged, and cut into parts of at least kSumRowsMin while the grid is
@@ -178,11 +176,10 @@ struct AttendSpace {
 };
 
 struct WeightsSpace {
-  int chunk, chunks, mt, row_blocks;  // the passes with rows in registers
-  bool stream_keys;    // the sums are one of them; else with keys in registers:
-  int tiles;           // ... 16-token tiles per wave
-  int blocks;          // ... token blocks of the longest sequence
+  int chunk, chunks, mt, row_blocks;  // the log-sums: rows in registers
+  int tiles;           // the sums: 16-token tiles per wave, keys in registers
   int held;            // rows that stay in LDS: tokens per workgroup (else 0)
+  int blocks;          // token blocks of the longest sequence
   int row_splits;      // parts the rows of the sums are cut into
   size_t ml;           // float2 [U][R][chunks]
   size_t lse;          // float [U][R]

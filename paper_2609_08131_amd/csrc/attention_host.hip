@@ -77,15 +77,13 @@ jacap_status check_attend(const jacap_config* cfg, const jacap_batch* batch,
 }
 
 // How the passes over rows and tokens of the weights are cut; `o` the
-// workspace's size so far. The chunks of the passes with rows in registers are one round
-// of the chip (fp32 rows, 32768 tokens: 92 us, 102 with chunks of half the size; five
-// sequences of 100 to 30000 tokens 120 and 141, equal long ones the same). The sums of
-// few rows stream the keys past the rows, as the log-sums do (log-sums and sums of 4
-// rows, 131072 tokens, 8 heads: 89 us streaming keys, 121 holding them); more rows
-// stay in LDS, a stretch of tokens passing them (256 rows, 4 layers of 131072 tokens:
-// 718 us with the log-sums, 865 with the rows staged for every 256 tokens; 100 rows,
-// 2 layers of 65536: 111 and 141; 256 rows of 1000 tokens 26.7 and 25.6, from the split
-// of their rows); and more than fit there are staged, in parts while the grid is small.
+// workspace's size so far. The chunks of the log-sums are one round of the chip (fp32
+// rows, 32768 tokens: 92 us, 102 with chunks of half the size; five sequences of 100 to
+// 30000 tokens 120 and 141, equal long ones the same). The rows of the sums stay
+// in LDS, a stretch of tokens passing them (256 rows, 4 layers of 131072 tokens: 718 us
+// with the log-sums, 865 with the rows staged for every 256 tokens; 100 rows, 2 layers of
+// 65536: 111 and 141; 256 rows of 1000 tokens 26.7 and 25.6, from the split of their rows);
+// more than fit there are staged, in parts while the grid is small.
 void layout_sum(const Geo& g, const Attn& at, bool bf16, WeightsSpace* w, size_t* o) {
   const int64_t LHT = (int64_t)g.L * g.H * g.T;
   const int tiles = (at.R + 15) / 16;
@@ -97,14 +95,13 @@ void layout_sum(const Geo& g, const Attn& at, bool bf16, WeightsSpace* w, size_t
   w->tiles = bf16 ? kSumTilesBf16 : kSumTilesFp32;
   const int tokens = 64 * w->tiles;
   w->blocks = (g.maxn + tokens - 1) / tokens;
-  w->stream_keys = tiles <= (bf16 ? kStreamTilesBf16 : kStreamTilesFp32);
   w->held = 0;
   w->row_splits = 1;
-  if (!w->stream_keys && at.R <= held_rows(g.D * (bf16 ? 2 : 4))) {
+  if (at.R <= held_rows(g.D * (bf16 ? 2 : 4))) {
     const int64_t per = (LHT / kHeldBlocks + tokens - 1) / tokens * tokens;
     w->held = (int)std::min<int64_t>(std::max<int64_t>(per, tokens), 1 << 20);
     w->blocks = (g.maxn + w->held - 1) / w->held;
-  } else if (!w->stream_keys) {
+  } else {
     const int64_t grid = std::max<int64_t>(1, LHT / tokens);
     w->row_splits =
         (int)std::max<int64_t>(1, std::min<int64_t>(kSumBlocks / grid, at.R / kSumRowsMin));

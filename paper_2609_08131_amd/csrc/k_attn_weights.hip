@@ -53,15 +53,10 @@ __device__ __forceinline__ float decayed(const Attn& at, float old, float sum) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows in registers, keys streamed. A workgroup takes 16 MT rows of a unit and a
-// chunk of its tokens; the waves take the chunk's 16-token steps in turn.
-//
-// SUM = false, the rows' lse: each lane keeps a maximum and sum of its own (its
-// row's tokens 4 q .. 4 q + 3), joined at the end.
-// SUM = true, the tokens' weights from the rows' known lse, for rows of one block
-// (the other way round a workgroup would load its keys for a handful of row
-// tiles). A step's weights are added over the row tiles in each lane, then
-// over the 16 lanes that hold a tile's rows.
+// The rows' lse: rows in registers, keys streamed. A workgroup takes 16 MT rows of a
+// unit and a chunk of its tokens; the waves take the chunk's 16-token steps in turn.
+// Each lane keeps a maximum and sum of its own (its row's tokens 4 q .. 4 q + 3), joined
+// at the end.
 //
 // The loop holds a step's logits, and forms the next step's tile by tile in their
 // place as they are added: no branch between, so that a tile's products run beside
@@ -72,14 +67,12 @@ constexpr int kFlush = 8;
 template <typename T>
 struct RowArgs {
   const T *q, *k;
-  float* acc;        // empty slots; SUM: updated
-  const float* lse_in;    // SUM: [B][L][H_q][w]
-  float* lse;        // else [B][L][H_q][w], written here with one chunk
+  const float* acc;  // empty slots
+  float* lse;        // [B][L][H_q][w], written here with one chunk
   float2* ml;        // ... or [U][R][chunks]
-  uint32_t* status;  // or null
 };
 
-template <typename T, int D, int MT, bool SUM>
+template <typename T, int D, int MT>
 __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, RowArgs<T> p,
                                                                 int chunk, int chunks,
                                                                 int row_blocks) {
@@ -101,12 +94,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
     pmin = rr0 % w;
     pmax = (rr1 - 1) % w;
   }
-  // (the sums pass every token: those that no row sees decay)
-  const int limit = at.causal && !SUM ? min(un.n, first + pmax + 1) : un.n;
+  const int limit = at.causal ? min(un.n, first + pmax + 1) : un.n;
   const int all = at.causal ? first + pmin + 1 : un.n;  // every row sees the tokens below
   const int t0 = split * chunk, t1 = min(limit, t0 + chunk);
 
-  // Minus the lane's maximum, its sum; SUM: minus lse, the row's weight. The sum is
+  // Minus the lane's maximum, and its sum, which is
   // taken by kFlush steps first: added one by one to that of a token which dominates the
   // row, most of the others' small weights would be lost to rounding, always to the
   // same side (a 128K window's accumulators off by 2e-6 relative, 2e-7 so).
@@ -119,25 +111,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
   }
   if (t0 < t1) {
     uint4 qf[MT][NP];
-    int last[MT];      // position of the lane's row of each tile; SUM: -1 if it adds nothing
-    bool dead = false;
+    int last[MT];  // position of the lane's row of each tile
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int r = rr0 + 16 * i + m, rc = min(r, R - 1);
-      bool used = r < R;
-      if constexpr (SUM) {
-        const int pos = rc % w;
-        const float ls = p.lse_in[((int64_t)un.b * g.L + un.l) * g.Hq * w + (int64_t)un.h * R + rc];
-        const float weight = at.row_weight ? at.row_weight[(int64_t)un.b * w + pos] : 1.0f;
-        used = used && weight != 0.0f && ls != -INFINITY;
-        nref[i] = used ? -ls * kLog2e : 0.0f;
-        l[i] = used ? weight : 0.0f;
-        dead |= !used;
-      }
-      load_row<T, D>(g, unit_queries(g, un, p.q), rc, used, qg, qf[i]);
-      last[i] = SUM && !used ? -1 : at.causal ? first + rc % w : INT32_MAX;
+      load_row<T, D>(g, unit_queries(g, un, p.q), rc, r < R, qg, qf[i]);
+      last[i] = at.causal ? first + rc % w : INT32_MAX;
     }
-    const bool some_dead = SUM && __ballot(dead) != 0;
     const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
     const int32_t ks = (int32_t)(g.kst * sizeof(T));
     const int64_t tr = token_row(g, un) + t0;
@@ -165,69 +145,48 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
     // takes the keys of the one after that.
     auto step = [&](const Keys& next, Keys& far) {
       const uint32_t vis = ((1u << min(16, t1 - r0)) - 1) & ~(uint32_t)__ballot(sign < 0.0f);
-      const float old = sign;
       sign = next.a;
       load(far, r0 + 128);
-      // SUM leaves hidden tokens out where it writes; rows that add nothing must not
-      // meet a key that is not finite
-      if ((!SUM && vis != 0xFFFFu) || r0 + 16 > all || some_dead) {
+      if (vis != 0xFFFFu || r0 + 16 > all) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int j = 4 * qg + e;
-            z[i][e] = (SUM || (vis >> j & 1)) && r0 + j <= last[i] ? z[i][e] : -INFINITY;
+            z[i][e] = (vis >> j & 1) && r0 + j <= last[i] ? z[i][e] : -INFINITY;
           }
       }
-      if constexpr (!SUM) {
-        float top[MT], over = kNoMax;
+      float top[MT], over = kNoMax;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        top[i] = max3(max3(z[i][0], z[i][1], z[i][2]), z[i][3], z[i][3]);
+        over = max3(over, __builtin_fmaf(top[i], at.c, nref[i]), over);
+      }
+      if (__ballot(over > kLazyMax) != 0) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          top[i] = max3(max3(z[i][0], z[i][1], z[i][2]), z[i][3], z[i][3]);
-          over = max3(over, __builtin_fmaf(top[i], at.c, nref[i]), over);
-        }
-        if (__ballot(over > kLazyMax) != 0) {
-#pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            const float now = fmaxf(-nref[i], top[i] * at.c), f = exp2_fast(-nref[i] - now);
-            l[i] *= f;
-            li[i] *= f;
-            nref[i] = -now;
-          }
-        }
-        if ((++steps & (kFlush - 1)) == 0) {
-#pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            l[i] += li[i];
-            li[i] = 0.0f;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          float y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = exp2_fast(__builtin_fmaf(z[i][e], at.c, nref[i]));
-          li[i] += (y[0] + y[1]) + (y[2] + y[3]);
-          z[i] = logits<T, D>(next.k, qf[i]);
-        }
-        interleave<W::kBf16, MT * NP>();
-      } else {
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sum[e] = __builtin_fmaf(exp2_fast(__builtin_fmaf(z[i][e], at.c, nref[i])), l[i], sum[e]);
-          z[i] = logits<T, D>(next.k, qf[i]);
-        }
-        interleave<W::kBf16, MT * NP>();
-        const float mine = tile_sum(sum, m);
-        const int j = 4 * qg + m;  // lanes m < 4 hold token j; its accumulator is lane j's
-        const float oldj = __shfl(old, j & 15);
-        if (m < 4 && r0 + j < t1) {
-          if (!(oldj < 0.0f)) p.acc[tr + (r0 - t0 + j)] = decayed(at, oldj, mine);
+          const float now = fmaxf(-nref[i], top[i] * at.c), f = exp2_fast(-nref[i] - now);
+          l[i] *= f;
+          li[i] *= f;
+          nref[i] = -now;
         }
       }
+      if ((++steps & (kFlush - 1)) == 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          l[i] += li[i];
+          li[i] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = exp2_fast(__builtin_fmaf(z[i][e], at.c, nref[i]));
+        li[i] += (y[0] + y[1]) + (y[2] + y[3]);
+        z[i] = logits<T, D>(next.k, qf[i]);
+      }
+      interleave<W::kBf16, MT * NP>();
       r0 += 64;
     };
     while (r0 < t1) {
@@ -235,10 +194,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
       if (r0 >= t1) break;
       step(ka, kb2);
     }
-  }
-  if constexpr (SUM) {
-    if (blockIdx.x == 0 && p.status) write_status(g, p.status);
-    return;
   }
   __shared__ float sm[4][16 * MT], sl[4][16 * MT];
 #pragma unroll
@@ -288,32 +243,30 @@ __global__ __launch_bounds__(kThreads) void attn_lse_join_kernel(Geo g, Attn at,
     lse[ur] = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
 }
 
-template <typename T, int D, int MT, bool SUM>
+template <typename T, int D, int MT>
 static hipError_t rows_typed(const AttnLaunch& A, const WeightsSpace& w, const RowArgs<T>& p) {
   const Geo& g = A.base.geo;
-  attn_rows_kernel<T, D, MT, SUM>
+  attn_rows_kernel<T, D, MT>
       <<<(unsigned)((int64_t)g.U * w.row_blocks * w.chunks), kThreads, 0, A.base.stream>>>(
           g, A.at, p, w.chunk, w.chunks, w.row_blocks);
   return hipGetLastError();
 }
 
-template <typename T, int D, bool SUM>
+template <typename T, int D>
 static hipError_t rows_tiles(const AttnLaunch& A, const WeightsSpace& w, const RowArgs<T>& p) {
   if constexpr (sizeof(T) == 2) {
-    if constexpr (!SUM)
-      if (w.mt == 8) return rows_typed<T, D, 8, SUM>(A, w, p);
-    if (w.mt == 4) return rows_typed<T, D, 4, SUM>(A, w, p);
+    if (w.mt == 8) return rows_typed<T, D, 8>(A, w, p);
+    if (w.mt == 4) return rows_typed<T, D, 4>(A, w, p);
   }
-  return rows_typed<T, D, 2, SUM>(A, w, p);
+  return rows_typed<T, D, 2>(A, w, p);
 }
 
 template <typename T, int D>
 static hipError_t lse_typed(const AttnLaunch& A, const WeightsSpace& w, const void* q, const void* k,
                             const float* acc, float* lse) {
   const Geo& g = A.base.geo;
-  RowArgs<T> p{(const T*)q, (const T*)k, const_cast<float*>(acc), nullptr, lse,
-               ws_ptr<float2>(A.base.wsp, w.ml), nullptr};
-  const hipError_t e = rows_tiles<T, D, false>(A, w, p);
+  RowArgs<T> p{(const T*)q, (const T*)k, acc, lse, ws_ptr<float2>(A.base.wsp, w.ml)};
+  const hipError_t e = rows_tiles<T, D>(A, w, p);
   if (e != hipSuccess || w.chunks == 1) return e;
   const int64_t rows = (int64_t)g.U * A.at.R;
   attn_lse_join_kernel<<<(unsigned)((rows + 15) / 16), kThreads, 0, A.base.stream>>>(
@@ -722,10 +675,7 @@ static hipError_t sum_typed(const AttnLaunch& A, const WeightsSpace& w, const vo
   const Geo& g = A.base.geo;
   float* part = ws_ptr<float>(A.base.wsp, w.part);
   hipError_t e;
-  if (w.stream_keys) {
-    e = rows_tiles<T, D, true>(A, w, RowArgs<T>{(const T*)q, (const T*)k, acc, lse, nullptr, nullptr,
-                                                status});
-  } else if (w.held) {
+  if (w.held) {
     attn_sum_held_kernel<T, D, NT>
         <<<(unsigned)((int64_t)g.U * std::max(1, w.blocks)), kThreads, 0, A.base.stream>>>(
             g, A.at, SumArgs<T>{(const T*)q, (const T*)k, lse, acc, nullptr, status}, w.held);
