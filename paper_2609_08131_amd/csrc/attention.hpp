@@ -33,9 +33,10 @@ constexpr int kJoinFew = 16;           // pieces of a row that one group of thre
 constexpr int kJoinRows = 1024;        // rows of a batch up to which a workgroup joins one
 constexpr int kJoinTokens = 1024;     // tokens per workgroup accumulating from kept logits
 // The log-sums, rows in registers: 16-row tiles per workgroup, at most, tokens,
-// and workgroups (two per compute unit).
+// and workgroups (two per compute unit); with fewer than kRowsSmall tokens each, the
+// batch is small.
 constexpr int kRowTilesBf16 = 8, kRowTilesFp32 = 2;
-constexpr int kRowsChunk = 16384, kRowsChunkMin = 256, kRowsBlocks = 512;
+constexpr int kRowsChunk = 16384, kRowsChunkMin = 256, kRowsBlocks = 512, kRowsSmall = 1024;
 // The accumulation: 16-token tiles per wave (their keys in registers). The rows of a
 // unit, up to 64 KiB of them, stay in LDS for one of kHeldBlocks stretches of the tokens;
 // more are staged, and cut into parts of at least kSumRowsMin while the grid is

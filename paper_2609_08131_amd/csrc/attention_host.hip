@@ -79,7 +79,10 @@ jacap_status check_attend(const jacap_config* cfg, const jacap_batch* batch,
 // How the passes over rows and tokens of the weights are cut; `o` the
 // workspace's size so far. The chunks of the log-sums are one round of the chip (fp32
 // rows, 32768 tokens: 92 us, 102 with chunks of half the size; five sequences of 100 to
-// 30000 tokens 120 and 141, equal long ones the same). The rows of the sums stay
+// 30000 tokens 120 and 141, equal long ones the same); small batches take fewer rows a
+// workgroup and half a round of longer chunks, as the rows' loads and the join of the
+// chunks weigh more (128 rows of 8192 tokens 21.2 us, 23.7 otherwise; of 16384 29.9 and 35.3;
+// of 32768 42.9 and 45.9; 64 rows of 8192 tokens 17.1 and 16.9). The rows of the sums stay
 // in LDS, a stretch of tokens passing them (256 rows, 4 layers of 131072 tokens: 718 us
 // with the log-sums, 865 with the rows staged for every 256 tokens; 100 rows, 2 layers of
 // 65536: 111 and 141; 256 rows of 1000 tokens 26.7 and 25.6, from the split of their rows);
@@ -88,8 +91,15 @@ void layout_sum(const Geo& g, const Attn& at, bool bf16, WeightsSpace* w, size_t
   const int64_t LHT = (int64_t)g.L * g.H * g.T;
   const int tiles = (at.R + 15) / 16;
   w->mt = !bf16 ? kRowTilesFp32 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : kRowTilesBf16;
-  w->row_blocks = (tiles + w->mt - 1) / w->mt;
-  const int64_t per_block = (LHT * w->row_blocks / kRowsBlocks + 63) / 64 * 64;
+  auto cut = [&](int blocks) {
+    w->row_blocks = (tiles + w->mt - 1) / w->mt;
+    return (LHT * w->row_blocks / blocks + 63) / 64 * 64;
+  };
+  int64_t per_block = cut(kRowsBlocks);
+  if (per_block < kRowsSmall) {
+    w->mt = std::min(w->mt, 4);
+    per_block = cut(kRowsBlocks / 2);
+  }
   w->chunk = (int)std::max<int64_t>(kRowsChunkMin, std::min<int64_t>(per_block, kRowsChunk));
   w->chunks = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
   w->tiles = bf16 ? kSumTilesBf16 : kSumTilesFp32;
