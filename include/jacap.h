@@ -438,13 +438,14 @@ jacap_status jacap_attn_weights(const jacap_config* cfg, const jacap_batch* batc
 /* Eviction by accumulated weight: jacap_select's rule (weight descending,
  * position ascending, NaN lowest, cfg->protect_last) on acc over the n_b
  * tokens of every sequence, then jacap_compact, and the kept tokens'
- * accumulators with them. Empty slots rank below every token; where fewer than
- * budget_k tokens are left, they are kept as empty slots.
+ * accumulators with them. Empty slots rank below every token of a weight that is
+ * not NaN; where fewer than budget_k tokens are left, they are kept as empty slots.
  *   idx     : int32 [B][L][H_kv][budget_k], as jacap_select.
  *   k_out, v_out : as jacap_compact (the batch's out strides).
  *   acc_out : float, entry j of unit (b, l, h) at b*a_stride_seq +
  *             l*a_stride_layer + h*a_stride_head + j (any strides >= 0); the
- *             entries past min(budget_k, n_b) are -1 (empty slots).
+ *             entries past min(budget_k, n_b) are -1 (empty slots). Must not
+ *             overlap acc.
  * attn: live_lens and the a strides are read. No workspace. */
 jacap_status jacap_evict_weighted(const jacap_config* cfg, const jacap_batch* batch,
                                   const jacap_attention* attn, const float* acc, const void* k,
