@@ -359,7 +359,7 @@ __device__ __forceinline__ uint32_t radix_rank(KeyAt key_at, int cnt, uint32_t r
 // General path: radix select over the scores, then an ordered emission pass by ballots
 // (20 units of 93567 tokens of which all but 346 are empty slots, keeping 349, with the
 // path before it: 370 us with one atomic per key and a contiguous segment per thread, 134
-// now).
+// now; 256 units of 131072 keeping 20000, with the evicted lists: 869 and 290).
 template <class C, int DIR>
 __device__ __forceinline__ void select_general(const RankedScores<DIR>& rs, int kk,
                                                const SelOut<DIR>& out, SelShared<C>& sh) {
