@@ -78,12 +78,17 @@ struct Row {
   static constexpr int kBlocks = kVLoads * kVec;         // 16-channel blocks of the output
 };
 
-// The larger of three, as the instruction takes them: fmaxf would first quiet each
-// operand that comes out of an MFMA, one instruction each.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+// The largest of four logits as an MFMA leaves them. The middle of a, b and +inf is the
+// larger of a and b (of a NaN and a number, the number). fmaxf would first quiet each
+// operand that comes out of an MFMA, one instruction each, and so would this if the compiler
+// knew the infinity. The maximum itself is not written as assembly: the wait states between
+// an MFMA and a vector instruction that reads its result are the compiler's to insert,
+// and it does so for the instructions that it knows only.
+__device__ __forceinline__ float max4(const f32x4& z) {
+  float inf = INFINITY;
+  asm("" : "+s"(inf));
+  const float a = __builtin_amdgcn_fmed3f(z[0], z[1], inf);
+  return __builtin_amdgcn_fmed3f(__builtin_amdgcn_fmed3f(a, z[2], inf), z[3], inf);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -692,17 +692,28 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
             z[i][t][e] = see ? z[i][t][e] : -INFINITY;
           }
     }
-    float top[MT], over = kNoMax;
+    // The exponents against the maxima so far, which the largest of them may raise. (Taken of
+    // the logits themselves, the maximum would cost a quieting instruction for each.)
+    float over = kNoMax;
+    f32x4 y[MT][2];
+    auto exponents = [&](int i) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[i][t][e] = __builtin_fmaf(z[i][t][e], at.c, -ref[i]);
+    };
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      top[i] = max3(max3(z[i][0][0], z[i][0][1], z[i][0][2]), max3(z[i][0][3], z[i][1][0], z[i][1][1]),
-                    max3(z[i][1][2], z[i][1][3], z[i][1][3]));
-      over = max3(over, __builtin_fmaf(top[i], at.c, -ref[i]), over);
+      exponents(i);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) over = fmaxf(over, y[i][t][e]);
     }
     if (__ballot(over > kLazyMax) != 0) {
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        float now = top[i] * at.c;
+        float now = fmaxf(max4(z[i][0]), max4(z[i][1])) * at.c;
         now = fmaxf(now, __shfl_xor(now, 16));
         now = fmaxf(now, __shfl_xor(now, 32));
         now = fmaxf(now, ref[i]);
@@ -711,6 +722,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
         l[i] *= f;
 #pragma unroll
         for (int b = 0; b < NB; ++b) o[i][b] *= f;
+        exponents(i);
       }
     }
     bf8 pb[MT];
@@ -720,7 +732,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          z[i][t][e] = exp2_fast(__builtin_fmaf(z[i][t][e], at.c, -ref[i]));
+          z[i][t][e] = exp2_fast(y[i][t][e]);
           pb[i][4 * t + e] = (__bf16)z[i][t][e];
         }
 #pragma unroll

@@ -159,8 +159,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
       float top[MT], over = kNoMax;
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        top[i] = max3(max3(z[i][0], z[i][1], z[i][2]), z[i][3], z[i][3]);
-        over = max3(over, __builtin_fmaf(top[i], at.c, nref[i]), over);
+        top[i] = max4(z[i]);
+        over = fmaxf(over, __builtin_fmaf(top[i], at.c, nref[i]));
       }
       if (__ballot(over > kLazyMax) != 0) {
 #pragma unroll
