@@ -548,6 +548,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_held_kernel(Geo g, Attn 
   struct Meta { float lse, weight; };
   __shared__ Meta meta[ROWS];
   __shared__ int last_lds[ROWS];  // last position seen, -1: adds nothing
+  // The row tiles with a row that adds nothing: its logits are replaced, since 0 times the
+  // weight of a key that holds an infinity or NaN would not be 0.
+  __shared__ uint32_t dead_lds[ROWS / 16];
 
   if (begin < end) {
     const T* kb = p.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
@@ -582,8 +585,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_held_kernel(Geo g, Attn 
         meta[16 * h + m] = Meta{live ? lse * kLog2e : 0.0f, live ? weight : 0.0f};
         last_lds[16 * h + m] = !live ? -1 : at.causal ? first + pos : INT32_MAX;
       }
+      const bool any = __ballot(!live) != 0;
+      if (lane == 0) dead_lds[h] = any;
     }
     __syncthreads();
+    const uint32_t dead = (uint32_t)__ballot(lane < STAGE * stages && dead_lds[lane % (ROWS / 16)]);
 
     f32x4 sum[NT], z[NT];
     float ls = 0.0f, weight = 0.0f;
@@ -607,7 +613,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_held_kernel(Geo g, Attn 
     };
     int before = -1;  // the block whose last logits z holds
     for (; tok < end; tok += STEP) {
-      const bool masked = at.causal && tok + 16 * NT > first + 1;
+      const bool edge = at.causal && tok + 16 * NT > first + 1;
+      const uint32_t masked = edge ? ~0u : dead;  // row tiles
       for (int s = 0; s < stages; ++s) {
 #pragma unroll
         for (int x = 0; x < STAGE; ++x) {
@@ -629,13 +636,20 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_held_kernel(Geo g, Attn 
             entries(tok);
             before = tok;
           }
-          if (masked) {
-            const int last = last_lds[16 * h + m];
+          if (masked >> h & 1) {
+            if (edge) {
+              const int last = last_lds[16 * h + m];
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+              for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                z[t][e] = tok + 16 * t + 4 * qg + e <= last ? z[t][e] : -INFINITY;
+                for (int e = 0; e < 4; ++e)
+                  z[t][e] = tok + 16 * t + 4 * qg + e <= last ? z[t][e] : -INFINITY;
+            } else {
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[t][e] = me.weight != 0.0f ? z[t][e] : -INFINITY;
+            }
           }
           ls = me.lse;
           weight = me.weight;

@@ -37,3 +37,38 @@ def test_large_logits_of_windows(jacap, dtype, d, w, G, causal):
     c = Case([500, 31, 3000], w, dtype, d, H=1, G=G, holes=0.05, seed=9, spread=400.0)
     print(f"[large] {dtype} d{d} w{w} G{G}", flush=True)
     check_weights(jacap, c, causal)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("w,G,given", [(13, 5, False), (64, 1, False), (31, 2, True), (64, 4, True),
+                                       (100, 1, True), (300, 2, True), (300, 2, False)])
+def test_infinite_keys_that_every_row_gives_nothing(jacap, dtype, w, G, given):
+    """A visible token whose logits are -inf in every row receives 0, beside rows of
+    weight 0 and the padding of the last row tiles; rows in LDS and staged."""
+    c = Case([900, 40, 0, 17], w, dtype, 64, G=G, holes=0.1, spare=2, seed=17)
+    c.q[..., 5] = c.q[..., 5].abs() + 0.25
+    c.k[:, :, 7::13, 5] = -math.inf
+    rw = lse = None
+    if given:
+        rw = (torch.arange(4 * w, device="cuda").view(4, w) % 3 == 0).float() * 0.5
+        lse = 5.0 + torch.rand((4, 1, 2 * G, w), device="cuda")
+    acc = check_weights(jacap, c, not given, given=lse, row_weight=rw, decay=0.5)
+    assert torch.isfinite(acc).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("w,G", [(21, 2), (64, 1), (300, 2)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_rows_of_weight_zero_beside_non_finite_keys(jacap, dtype, w, G, value):
+    """Sequences none of whose rows has a weight keep their accumulators, whatever their
+    keys hold; the others' rows of weight 0 add nothing either."""
+    c = Case([900, 40, 300], w, dtype, 128, G=G, holes=0.1, seed=18)
+    c.k[:, :, 3:900:17] = value             # sequence 0, and one token of sequence 1
+    c.k[:, :, 905] = value
+    rw = torch.rand((3, w), device="cuda") + 0.5
+    rw[0] = 0.0
+    rw[1, ::2] = 0.0
+    lse = 5.0 + torch.rand((3, 1, 2 * G, w), device="cuda")
+    acc = check_weights(jacap, c, False, given=lse, row_weight=rw)
+    assert torch.equal(acc[:, :, :900], c.acc[:, :, :900])
+    assert torch.isfinite(acc[:, :, 940:]).all()
