@@ -290,7 +290,13 @@ hipError_t launch_attn_lse(const AttnLaunch& A, const WeightsSpace& w, const voi
 // buffers, the next rows requested a stage ahead). A lane adds the weights its
 // query row gives its tokens; the 16 lanes of a tile's rows are added at the
 // end. DRAFT: the tokens are the drafted ones, seen by the tree's mask.
+// The weights of a whole prompt are many and may be nearly equal (a token that every row
+// attends to), and one by one in fp32 they would round to the same side: R = 524288 rows of
+// weights near 0.9 lose 5e-5 of their sum, however exact each is. kSumFlush stages (of 64 rows
+// in bf16, 32 in fp32: at most 64 additions a lane) are summed in fp32, their sums in fp64.
 // ---------------------------------------------------------------------------
+constexpr int kSumFlush = 16;
+
 template <typename T>
 struct SumArgs {
   const T *q, *k;
@@ -301,7 +307,7 @@ struct SumArgs {
 };
 
 template <typename T, int D, int NT, bool DRAFT>
-__global__ __launch_bounds__(kThreads, 2) void attn_sum_kernel(Geo g, Attn at, SumArgs<T> p, int blocks,
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_sum_kernel(Geo g, Attn at, SumArgs<T> p, int blocks,
                                                             int row_splits) {
   using W = Row<T, D>;
   constexpr int NP = W::kPieces;
@@ -405,19 +411,32 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_kernel(Geo g, Attn at, S
     };
 
     // z: the logits of the last row tile, not added yet; its rows' lse and weight
+    // sum: the weights of the last kSumFlush stages, by row; total: of those before, each
+    // token's read and written by one lane. In LDS, and the registers bounded: three waves
+    // of d = 64 share a SIMD so (a prompt of 8192: 480 us, 512 with total in registers).
     f32x4 sum[NT], z[NT];
+    __shared__ double total[64 * NT];
     float ls = 0.0f, weight = 0.0f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       z[t] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     }
+    auto flush = [&](bool first) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        double& x = total[(wave * NT + t) * 16 + 4 * qg + (m & 3)];
+        const float mine = tile_sum(sum[t], m);
+        if (m < 4) x = first ? (double)mine : x + (double)mine;
+        sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    };
     auto add = [&](int t) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         sum[t][e] = __builtin_fmaf(exp2_fast(__builtin_fmaf(z[t][e], at.c, -ls)), weight, sum[t][e]);
     };
-    int buf = 0;
+    int buf = 0, done = 0;
     seek(part * per);
     skip();
     bool more = stage < stage1;
@@ -491,6 +510,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_kernel(Geo g, Attn at, S
         }
       }
       if (more) store(buf ^ 1);
+      if ((++done & (kSumFlush - 1)) == 0) flush(done == kSumFlush);
       __syncthreads();
       buf ^= 1;
     }
@@ -498,7 +518,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_kernel(Geo g, Attn at, S
     for (int t = 0; t < NT; ++t) add(t);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const float mine = tile_sum(sum[t], m);
+      float mine = tile_sum(sum[t], m);
+      if (done >= kSumFlush && m < 4)
+        mine = (float)(total[(wave * NT + t) * 16 + 4 * qg + (m & 3)] + (double)mine);
       const int j = tok + 16 * t + 4 * qg + m;
       if (m < 4 && j < n) {
         if constexpr (DRAFT) {
@@ -678,9 +700,9 @@ __global__ __launch_bounds__(kThreads) void attn_sum_join_kernel(Geo g, Attn at,
   if (t >= un.n) return;
   const float old = acc[tr + t];
   if (old < 0.0f) return;
-  float sum = 0.0f;
-  for (int s = 0; s < row_splits; ++s) sum += part[s * pitch + tr + t];
-  acc[tr + t] = decayed(at, old, sum);
+  double sum = 0.0;
+  for (int s = 0; s < row_splits; ++s) sum += (double)part[s * pitch + tr + t];
+  acc[tr + t] = decayed(at, old, (float)sum);
 }
 
 template <typename T, int D, int NT>

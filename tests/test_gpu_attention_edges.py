@@ -72,3 +72,28 @@ def test_rows_of_weight_zero_beside_non_finite_keys(jacap, dtype, w, G, value):
     acc = check_weights(jacap, c, False, given=lse, row_weight=rw)
     assert torch.equal(acc[:, :, :900], c.acc[:, :, :900])
     assert torch.isfinite(acc[:, :, 940:]).all()
+
+
+@pytest.mark.parametrize("dtype,T,w,G", [(BF, 132000, 131072, 4), (F32, 66000, 32768, 4), (BF, 300, 131072, 4),
+                                         (F32, 130, 65536, 4)])
+@pytest.mark.parametrize("weight", [0.9, 0.5])
+def test_sums_of_many_nearly_equal_weights(jacap, dtype, T, w, G, weight):
+    """Every row gives every token nearly the same weight (keys of 0, lse given): the
+    bound does not grow with the rows. One row part, and many (short caches).
+
+    A weight: lse log2(e) is rounded (u |lse|), and so is the exponent's argument; the
+    exponential is within one unit, 2 u. At most 64 additions of a lane in fp32, then fp64
+    sums rounded to fp32 at most twice, the 16 lanes' tree 4 u, the part's rounding and the
+    last addition's: 2 |lse| u + 2 u + 64 u + 2 u + 4 u + 2 u < 76 u for |lse| < 1."""
+    q = torch.zeros((1, 1, G, w, 64), dtype=dtype, device="cuda")
+    k = torch.zeros((1, 1, T, 64), dtype=dtype, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lse = -torch.log(weight + 0.001 * torch.rand((1, 1, G, w), generator=gen, device="cuda"))
+    acc = torch.zeros((1, 1, T), device="cuda")
+    prob = jacap.prepare_attn_weights(q, k, torch.tensor([0, T], dtype=torch.int32, device="cuda"), [T],
+                                      jacap.AttentionParams(causal=False))
+    jacap.run_attn_weights(prob, q, k, acc, lse=lse)
+    want = float(torch.exp(-lse.double()).sum())
+    worst = float((acc.double() - want).abs().max()) / want
+    print(f"[sums] {dtype} T{T} R{G * w} weight {weight}: {worst:.3e}", flush=True)
+    assert worst <= 76 * U
