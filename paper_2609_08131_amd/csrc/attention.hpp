@@ -158,7 +158,9 @@ __device__ __forceinline__ void write_status(const Geo& g, uint32_t* status) {
 // exp2(ref - larger) are 0. It is raised only when a logit exceeds it by more
 // than kLazyMax, so most steps rescale nothing; the weights stay below 2^8, far
 // inside fp32 and bf16.
-constexpr float kNoMax = -3.402823466e+38f;
+// A logit of +inf raises it to kTop only, so that its own weight is infinite, not NaN: the sum
+// and its logarithm are then +inf, as the formula has them.
+constexpr float kNoMax = -3.402823466e+38f, kTop = -kNoMax;
 constexpr float kLazyMax = 8.0f;
 
 // ---------------------------------------------------------------------------

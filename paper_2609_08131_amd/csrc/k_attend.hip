@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendParams<T> par
         float now = top[i] * at.c;
         now = fmaxf(now, __shfl_xor(now, 16));
         now = fmaxf(now, __shfl_xor(now, 32));
-        now = fmaxf(now, ref[i]);
+        now = fminf(fmaxf(now, ref[i]), kTop);
         const float f = exp2_fast(ref[i] - now);
         ref[i] = now;
         l[i] *= f;
@@ -716,7 +716,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
         float now = fmaxf(max4(z[i][0]), max4(z[i][1])) * at.c;
         now = fmaxf(now, __shfl_xor(now, 16));
         now = fmaxf(now, __shfl_xor(now, 32));
-        now = fmaxf(now, ref[i]);
+        now = fminf(fmaxf(now, ref[i]), kTop);
         const float f = exp2_fast(ref[i] - now);
         ref[i] = now;
         l[i] *= f;
@@ -1094,10 +1094,10 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     const Pieces pc = pieces_of(g, jg, p.before, un, u, rc, R);
     float top = kNoMax, l = 0.0f;
     if (pc.n == 1) {
-      const float ls = p.lse[(int64_t)u * R + rc];
+      const float ls = p.lse[(int64_t)u * R + rc] * kLog2e;
       if ((tid & 15) == 0 && ls != -INFINITY) {
-        top = ls * kLog2e;
-        l = 1.0f;
+        top = fminf(ls, kTop);
+        l = exp2_fast(ls - top);  // 1, or as infinite or NaN as ls
       }
     } else {
       for (int s = tid & 15; s < pc.n; s += 16) {

@@ -165,7 +165,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Geo g, Attn at, 
       if (__ballot(over > kLazyMax) != 0) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          const float now = fmaxf(-nref[i], top[i] * at.c), f = exp2_fast(-nref[i] - now);
+          const float now = fminf(fmaxf(-nref[i], top[i] * at.c), kTop);
+          const float f = exp2_fast(-nref[i] - now);
           l[i] *= f;
           li[i] *= f;
           nref[i] = -now;

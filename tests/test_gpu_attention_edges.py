@@ -97,3 +97,31 @@ def test_sums_of_many_nearly_equal_weights(jacap, dtype, T, w, G, weight):
     worst = float((acc.double() - want).abs().max()) / want
     print(f"[sums] {dtype} T{T} R{G * w} weight {weight}: {worst:.3e}", flush=True)
     assert worst <= 76 * U
+
+
+def _infinite_logits(c):
+    """Tokens whose logits are +inf in the even heads' rows and -inf in the odd ones'."""
+    c.q[..., 5] = c.q[..., 5].abs() + 0.25
+    c.q[:, :, 1::2, :, 5] *= -1.0
+    c.k[:, :, 7:300:97, 5] = math.inf
+    return c
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("S,G", [(1, 2), (5, 3), (20, 2), (40, 2), (130, 2)])
+@pytest.mark.parametrize("lens", [[300, 3, 40], [4000, 900, 31]])
+def test_infinite_logits(jacap, dtype, d, S, G, lens):
+    """lse +inf and out NaN in the rows that have one, whose weights are 0 but for the
+    infinite token's own, NaN; the other rows are as without that token."""
+    c = _infinite_logits(Case(lens, S, dtype, d, H=2, G=G, holes=0.05, tree="tree" if S > 1 else None, seed=19))
+    prob, acc = run_attend(jacap, c, True, True, decay=0.5)
+    assert torch.isposinf(prob.lse).any() and torch.isfinite(prob.lse).any()
+    check_attend(c, prob, acc, True, True, decay=0.5)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("w,G,causal", [(1, 2, True), (16, 2, False), (64, 4, True), (300, 2, True)])
+@pytest.mark.parametrize("lens", [[300, 3, 40], [20000, 900, 31]])
+def test_infinite_logits_of_windows(jacap, dtype, w, G, causal, lens):
+    c = _infinite_logits(Case(lens, w, dtype, 64, H=2, G=G, holes=0.05, seed=20))
+    check_weights(jacap, c, causal, decay=0.5)
