@@ -361,6 +361,15 @@ jacap_status jacap_greedy(const jacap_config* cfg, const jacap_batch* batch, con
  * is taken as empty. Everything these calls read on the device may change
  * between the replays of a captured graph.
  *
+ * Limits (JACAP_ERR_UNSUPPORTED beyond; split the batch by layers or sequences):
+ * total_tokens up to 2^31 - 1 - 2^21; with U = num_seqs x num_layers x
+ * num_kv_heads units of R = (num_q_heads / num_kv_heads) x window rows, U R up to
+ * 2^24 - 1 in jacap_attend and 2^28 - 1 in jacap_attn_weights; and grids of at most
+ * 2^24 - 1 workgroups, of which the longest sequence, min(max_seq_len,
+ * total_tokens), takes one per unit and 1024 tokens in jacap_attend, and where the
+ * weights of more rows than 256 (fp32 at d = 128: 128) are summed one per unit and 256
+ * tokens (fp32: 128).
+ *
  * cfg->temperature, ridge, cov_mode, ridge_mode and gqa_mode are not read for
  * their meaning here (the entry points check them as everywhere), and budget_k,
  * protect_last and the batch's out strides only by the eviction calls. Logits,

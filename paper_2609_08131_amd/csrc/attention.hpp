@@ -45,6 +45,7 @@ constexpr int kSumTilesBf16 = 4, kSumTilesFp32 = 2;
 constexpr int held_rows(int row_bytes) { return row_bytes <= 256 ? 256 : 128; }
 constexpr int kHeldBlocks = 512;
 constexpr int kSumRowsMin = 128, kSumBlocks = 1024;
+constexpr int64_t kMaxTokens = INT32_MAX - (int64_t(1) << 21);  // cached rows of a (layer, KV head)
 constexpr int64_t kMaxGrid = (int64_t(1) << 24) - 1;  // workgroups of 256 threads in one launch
 
 // Device view of jacap_attention (and the launch's chunking).

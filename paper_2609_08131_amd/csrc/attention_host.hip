@@ -29,9 +29,14 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 // The descriptor and what every call shares. ws = null: no workspace is checked.
 jacap_status check(const jacap_config* cfg, const jacap_batch* batch, const jacap_attention* at,
                    void* stream, AttnLaunch* A) {
-  const jacap_status s = prepare_launch(cfg, batch, nullptr, 0, stream, &A->base);
+  if (!batch || !at) return JACAP_ERR_INVALID_ARG;
+  // No sequence is longer than all of them, whatever length the caller declares: what is cut
+  // and counted below (in 32 bits, up to a chunk past the end) follows the shorter.
+  jacap_batch b = *batch;
+  if (b.total_tokens > kMaxTokens) return JACAP_ERR_UNSUPPORTED;
+  b.max_seq_len = (int32_t)std::min<int64_t>(b.max_seq_len, std::max<int64_t>(b.total_tokens, 0));
+  const jacap_status s = prepare_launch(cfg, &b, nullptr, 0, stream, &A->base);
   if (s != JACAP_OK) return s;
-  if (!at) return JACAP_ERR_INVALID_ARG;
   if (!(at->scale > 0.0f) || !isfinite(at->scale * kLog2e)) return JACAP_ERR_INVALID_ARG;
   if (!(at->decay >= 0.0f && at->decay <= 1.0f)) return JACAP_ERR_INVALID_ARG;
   if ((at->accumulate | 1) != 1 || (at->causal | 1) != 1) return JACAP_ERR_INVALID_ARG;
@@ -128,6 +133,7 @@ bool sum_grid_ok(const Geo& g, const WeightsSpace& w) {
 jacap_status layout_weights(const AttnLaunch& A, bool bf16, WeightsSpace* w) {
   const Geo& g = A.base.geo;
   const int64_t UR = (int64_t)g.U * A.at.R;
+  if (UR / 16 > kMaxGrid) return JACAP_ERR_UNSUPPORTED;
   size_t o = 256;
   layout_sum(g, A.at, bf16, w, &o);
   w->lse = o;
@@ -135,7 +141,7 @@ jacap_status layout_weights(const AttnLaunch& A, bool bf16, WeightsSpace* w) {
   w->ml = o;
   if (w->chunks > 1) o = align256(o + 8 * (size_t)UR * w->chunks);
   w->total = o;
-  return UR / 16 > kMaxGrid || !sum_grid_ok(g, *w) ? JACAP_ERR_UNSUPPORTED : JACAP_OK;
+  return sum_grid_ok(g, *w) ? JACAP_OK : JACAP_ERR_UNSUPPORTED;
 }
 
 // sum: the accumulation's own cut, for accumulating from more rows than keep
@@ -143,6 +149,7 @@ jacap_status layout_weights(const AttnLaunch& A, bool bf16, WeightsSpace* w) {
 jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, WeightsSpace* sum) {
   const Geo& g = A.base.geo;
   const int64_t UR = (int64_t)g.U * A.at.R, LHT = (int64_t)g.L * g.H * g.T;
+  if (UR > kMaxGrid) return JACAP_ERR_UNSUPPORTED;
   size_t o = 256;
   w->mt = A.at.R <= 16 ? 1 : 2;
   w->rw = !bf16 || A.at.R <= kWideRows ? 0 : A.at.R <= 64 ? 2 : A.at.R <= 128 ? 4 : 8;

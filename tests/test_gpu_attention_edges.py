@@ -125,3 +125,33 @@ def test_infinite_logits(jacap, dtype, d, S, G, lens):
 def test_infinite_logits_of_windows(jacap, dtype, w, G, causal, lens):
     c = _infinite_logits(Case(lens, w, dtype, 64, H=2, G=G, holes=0.05, seed=20))
     check_weights(jacap, c, causal, decay=0.5)
+
+
+@pytest.mark.parametrize("dtype,S,G", [(BF, 1, 2), (BF, 40, 2), (F32, 9, 2), (BF, 130, 4)])
+@pytest.mark.parametrize("declared", [2 ** 31 - 1, 2 ** 31 - 1000, 10 ** 6])
+def test_declared_length_far_above_the_tokens(jacap, dtype, S, G, declared):
+    """max_seq_len is an upper bound, of any size: results as with the longest length."""
+    c = Case([3000, 0, 700], S, dtype, 64, H=2, G=G, holes=0.05, seed=23)
+    results = []
+    for longest in (3000, declared):
+        p = jacap.AttentionParams(accumulate=True)
+        prob = jacap.prepare_attend(c.q, c.k, c.v, c.kd, c.vd, c.offsets, c.rows, p)
+        wp = jacap.prepare_attn_weights(c.q, c.k, c.offsets, c.rows, p)
+        for x, size in ((prob, jacap.attend_workspace_size), (wp, jacap.attn_weights_workspace_size)):
+            x.batch.max_seq_len = longest
+            x.ws = torch.empty(size(x.cfg, x.batch, x.attn), dtype=torch.uint8, device="cuda")
+        acc = c.acc.clone()
+        jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd, acc=acc)
+        assert jacap.read_status(prob.ws) == 0
+        check_attend(c, prob, acc, True, True)
+        jacap.run_attn_weights(wp, c.q, c.k, acc)
+        assert jacap.read_status(wp.ws) == 0
+        results.append((wp.lse, acc))
+    (lse, acc), (lse2, acc2) = results
+    # (the chunks may differ: sums within their bounds, 3000 tokens, at most 520 rows)
+    assert torch.equal(torch.isfinite(lse), torch.isfinite(lse2))
+    f = torch.isfinite(lse)
+    assert float((lse[f] - lse2[f]).abs().max()) <= 2 * 3004 * U + 8 * U * float(lse[f].abs().max())
+    seen = acc >= 0
+    assert torch.equal(acc < 0, acc2 < 0)
+    assert float(((acc - acc2).abs() / acc.abs().clamp_min(1e-30))[seen].max()) <= 4 * (3004 + 524) * U
