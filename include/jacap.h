@@ -358,7 +358,8 @@ jacap_status jacap_greedy(const jacap_config* cfg, const jacap_batch* batch, con
  * of the cache, of which the first live_lens[b] hold tokens (n_b in what
  * follows); null = all of them. A length below 0 or above the rows raises
  * JACAP_FLAG_BAD_OFFSETS, as inconsistent offsets do, and the sequence's cache
- * is taken as empty. Everything these calls read on the device may change
+ * is taken as empty. The other sequences' results hold as long as their rows do not
+ * overlap. Everything these calls read on the device may change
  * between the replays of a captured graph.
  *
  * Limits (JACAP_ERR_UNSUPPORTED beyond; split the batch by layers or sequences):

@@ -172,11 +172,12 @@ struct AttendSpace {
   int spans;           // ... and workgroups; or
   int rw;              // waves of 32 rows that share the cache through LDS (0: none do),
   int chunk, splits;   // ... with tokens per workgroup, chunks of the longest sequence
+  int places;          // ... and pieces of a row of a (layer, KV head), at most
   int row_blocks;
   size_t before;       // int32 [B + 1]             groups of tokens before each sequence
   size_t ml;           // float2 [pieces]           (maximum, sum) of a row's piece
   size_t part;         // float  [pieces][D]        its unnormalised output; the pieces:
-                       // [2 spans][16 mt], or [U][R][splits]
+                       // [2 spans][16 mt], or [L][H][places R], a sequence's [R][its pieces]
   size_t lse;          // float  [U][R]
   size_t z;            // float  [L][H][tiles][R][16] kept logits (accumulating from few rows)
   size_t zd;           // float  [U][R][S]          ... and the drafted tokens'

@@ -155,7 +155,7 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
   w->rw = !bf16 || A.at.R <= kWideRows ? 0 : A.at.R <= 64 ? 2 : A.at.R <= 128 ? 4 : 8;
   const int rows = w->rw ? 32 * w->rw : 16 * w->mt;
   w->row_blocks = (A.at.R + rows - 1) / rows;
-  w->spans = 0;
+  w->spans = w->places = 0;
   w->chunk = w->splits = 1;
   int64_t pieces;
   if (w->rw) {
@@ -164,7 +164,11 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
     w->chunk = (int)std::min<int64_t>(std::max<int64_t>((per + 127) / 128 * 128, kWideChunkMin),
                                       1 << 20);
     w->splits = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
-    pieces = UR * w->splits;
+    // Bounded by the tokens: with a place for each chunk of the longest in every sequence,
+    // 64 sequences of which one has 131072 tokens would take 2 GB (252 rows, 8 KV heads;
+    // 100 MB so).
+    w->places = w->splits > 1 ? (int)(g.T / w->chunk) + g.B : 0;
+    pieces = (int64_t)g.L * g.H * w->places * A.at.R;
   } else {
     // no more spans than there can be work for
     const int64_t most = (LHT / kSpanMin + (int64_t)g.U * (1 + kUnitGroups)) * w->row_blocks;

@@ -85,6 +85,13 @@ __device__ __forceinline__ int64_t piece_of(int start, int quantum, int j) {
   const int w = start / quantum;
   return 2 * (int64_t)(w + j) + (j == 0 && start != w * quantum);
 }
+// Where the first of the n pieces of row r of a unit cut into chunks lies. A sequence's pieces,
+// [R][n], start behind those of t0 / chunk + b chunks of its (layer, KV head), which is room for
+// the sequences before it, whatever their lengths.
+__device__ __forceinline__ int64_t chunk_place(const Geo& g, const Unit& un, int places, int chunk, int R,
+                                               int r, int n) {
+  return (((int64_t)un.l * g.H + un.h) * places + un.t0 / chunk + un.b) * R + (int64_t)r * n;
+}
 // A sequence's first cache row and current length.
 __device__ __forceinline__ int2 sequence_rows(const Geo& g, int b) {
   const int32_t a = g.seq_off[b], e = g.seq_off[b + 1];
@@ -573,7 +580,8 @@ struct Wide {
 template <int D, int RW, bool HIDES>
 __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Attn at,
                                                                       AttendArgs<__bf16> p, int chunk,
-                                                                      int splits, int row_blocks) {
+                                                                      int splits, int row_blocks,
+                                                                      int places) {
   using T = __bf16;
   using W = Row<T, D>;
   using S_ = Wide<D, RW>;
@@ -874,11 +882,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
       __syncthreads();
     }
     if (grp > 0 || row[i] >= R) continue;
-    const int64_t ur = (int64_t)u * R + row[i];
+    const int64_t place = chunk_place(g, un, places, chunk, R, row[i], nsp) + split;
     const int head = row[i] / S, pos = row[i] - head * S;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     T* dst = p.out + un.b * at.os + un.l * at.ol + (int64_t)(un.h * g.G + head) * at.oh + pos * at.op;
-    float* part = p.part + (ur * splits + split) * D;
+    float* part = p.part + place * D;  // (only where there are pieces)
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       f32x4 val = o[i][b] * f;
@@ -895,7 +903,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void attend_wide_kernel(Geo g, Att
       }
     }
     if (qg == 0) {
-      if (splits > 1) p.ml[ur * splits + split] = float2{top, sum};
+      if (nsp > 1) p.ml[place] = float2{top, sum};
       if (nsp == 1 && p.lse)
         p.lse[(((int64_t)un.b * g.L + un.l) * g.Hq + un.h * g.G + head) * S + pos] =
             sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
@@ -926,7 +934,8 @@ static hipError_t attend_typed(const AttnLaunch& A, const AttendSpace& w, const 
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
-        kern<<<(unsigned)grid, kWideThreads, lds, A.base.stream>>>(g, A.at, p, w.chunk, w.splits, w.row_blocks);
+        kern<<<(unsigned)grid, kWideThreads, lds, A.base.stream>>>(g, A.at, p, w.chunk, w.splits, w.row_blocks,
+                                                                w.places);
         return hipGetLastError();
       };
       auto pick = [&](auto rw) {
@@ -988,12 +997,14 @@ struct Pieces {
 // spans > 0: attend_kernel's, in groups of `group` tokens and blocks of `rows` rows;
 // else attend_wide_kernel's chunks.
 struct JoinGeo {
-  int chunk, splits, spans, group, rows, row_blocks;
+  int chunk, places, spans, group, rows, row_blocks;
 };
 __device__ __forceinline__ Pieces pieces_of(const Geo& g, const JoinGeo& j, const int32_t* before,
                                             const Unit& un, int u, int r, int R) {
-  if (j.spans == 0)
-    return {max(1, (un.n + j.chunk - 1) / j.chunk), (int)(((int64_t)u * R + r) * j.splits), 0, 0, 0};
+  if (j.spans == 0) {
+    const int n = max(1, (un.n + j.chunk - 1) / j.chunk);
+    return {n, (int)chunk_place(g, un, j.places, j.chunk, R, r, n), 0, 0, 0};
+  }
   const int per_seq = g.L * g.H * j.row_blocks;
   const int q = span_quantum(before[g.B] * per_seq, j.spans, j.group);
   const int run = before[un.b + 1] - before[un.b], c = run - kUnitGroups;
@@ -1015,7 +1026,11 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     const int64_t ur = few ? min((int64_t)blockIdx.x * NG + grp, (int64_t)g.U * R - 1) : blockIdx.x;
     const int u = ur / R, r = ur - (int64_t)u * R;
     Unit un{u / (g.L * g.H), u / g.H % g.L, u % g.H};  // (of the group, not of the workgroup)
-    if (jg.spans == 0) un.n = sequence_rows(g, un.b).y;
+    if (jg.spans == 0) {
+      const int2 rows = sequence_rows(g, un.b);
+      un.t0 = rows.x;
+      un.n = rows.y;
+    }
     const Pieces pc = pieces_of(g, jg, p.before, un, u, r, R);
     // one piece: written by the first kernel (threads of a wave may hold different rows)
     if (pc.n == 1) return;
@@ -1154,7 +1169,7 @@ static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, void* ou
                 ws_ptr<int32_t>(ws, w.before), w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
                 w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, acc, acc_draft};
   const bool wide = w.rw > 0;
-  const JoinGeo jg{w.chunk, w.splits, wide ? 0 : w.spans, kGroup<T, D>, 16 * w.mt, w.row_blocks};
+  const JoinGeo jg{w.chunk, w.places, wide ? 0 : w.spans, kGroup<T, D>, 16 * w.mt, w.row_blocks};
   // Spans of a batch of many rows hold many units each, so a row has few pieces; of
   // few rows (at most a workgroup's worth per compute unit), as many as there are spans.
   const int64_t UR = (int64_t)g.U * A.at.R;

@@ -97,14 +97,19 @@ static void run(const Shape& s) {
     EXPECT(attend(p, ws) == JACAP_OK && stub::attention_calls[stub::kAttend] == 1);
     const jacap::AttendSpace& w = stub::attend;
     EXPECT(stub::attention.base.geo.maxn == n);
-    const size_t pieces = w.rw ? (size_t)(U * R * w.splits) : (size_t)2 * w.spans * 16 * w.mt;
+    const size_t pieces = w.rw ? (size_t)((int64_t)s.L * s.H * w.places * R) : (size_t)2 * w.spans * 16 * w.mt;
     EXPECT(w.before >= 4 && w.lse >= w.before + 4 * (size_t)(s.B + 1) && w.ml >= w.lse + 4 * (size_t)(U * R));
     EXPECT(w.part >= w.ml + 8 * pieces && w.z >= w.part + 4 * pieces * s.d && w.total <= ws);
     if (w.keep)
       EXPECT(w.zd >= w.z + 64 * (size_t)s.L * s.H * (size_t)(s.total / 16 + s.B + 1) * R &&
              w.total >= w.zd + 4 * (size_t)(U * R * s.rows));
-    if (w.rw) EXPECT((int64_t)w.chunk * w.splits >= n && 32 * w.rw * w.row_blocks >= R);
-    else EXPECT(w.spans >= 1 && 16 * w.mt * w.row_blocks >= R);
+    if (w.rw) {
+      EXPECT((int64_t)w.chunk * w.splits >= n && 32 * w.rw * w.row_blocks >= R);
+      // room for the chunks of any sequences, whatever their lengths; no more than they need
+      EXPECT(w.splits == 1 || w.places >= s.total / w.chunk + s.B);
+      EXPECT(w.ml + 4096 + (size_t)(s.total / w.chunk + s.B) * s.L * s.H * R * (8 + 4 * s.d) >= w.z);
+    }
+    if (!w.rw) EXPECT(w.spans >= 1 && 16 * w.mt * w.row_blocks >= R);
     const bool sums = accumulate && !w.keep;
     EXPECT(stub::attention_calls[stub::kDraftSum] == sums);
     EXPECT(stub::attention_calls[stub::kSum] == (sums && s.total > 0));

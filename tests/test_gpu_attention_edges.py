@@ -155,3 +155,13 @@ def test_declared_length_far_above_the_tokens(jacap, dtype, S, G, declared):
     seen = acc >= 0
     assert torch.equal(acc < 0, acc2 < 0)
     assert float(((acc - acc2).abs() / acc.abs().clamp_min(1e-30))[seen].max()) <= 4 * (3004 + 524) * U
+
+
+@pytest.mark.parametrize("S,G,spare", [(40, 1, 0), (40, 2, 300), (70, 4, 3)])
+def test_many_rows_of_unequal_sequences(jacap, S, G, spare):
+    """The pieces of a ragged batch: sequences of no, one, and several chunks, of any length
+    and order; rows reserved behind them."""
+    c = Case([0, 9000, 5, 257, 4000, 0, 256, 512, 1, 2300, 700, 6001], S, BF, 64, H=2, G=G, L=2, holes=0.05,
+             spare=spare, tree="tree", seed=24)
+    prob, acc = run_attend(jacap, c, True, True)
+    check_attend(c, prob, acc, True, True)
