@@ -548,8 +548,8 @@ def _strides(a, prefix: str, t: torch.Tensor) -> None:
 
 @dataclasses.dataclass
 class AttendProblem:
-    """Descriptors, outputs and workspace of jacap_attend for one batch. The
-    parameters' tensors are kept with it: the descriptors hold their addresses."""
+    """Descriptors, outputs and workspace of jacap_attend for one batch. A copy of
+    the parameters is kept with it, for their tensors: the descriptors hold their addresses."""
 
     cfg: Config
     batch: Batch
@@ -584,7 +584,8 @@ def prepare_attend(q, k, v, kd, vd, seq_offsets, seq_lens, params: AttentionPara
         if params.accumulate else None
     layout = {n: _layout(t) for n, t in (("q", q), ("k", k), ("v", v), ("kd", kd), ("vd", vd))}
     layout["acc"] = _acc_layout(k)
-    return AttendProblem(cfg, batch, attn, out, lse, acc_draft, ws, params, seq_offsets, layout)
+    return AttendProblem(cfg, batch, attn, out, lse, acc_draft, ws, dataclasses.replace(params),
+                         seq_offsets, layout)
 
 
 def _layout(t: torch.Tensor):
@@ -642,7 +643,8 @@ def prepare_attn_weights(q, k, seq_offsets, seq_lens, params: AttentionParams) -
     ws = _workspace(attn_weights_workspace_size(cfg, batch, attn), k.device)
     lse = torch.empty((B, L, Hq, w), dtype=torch.float32, device=k.device)
     layout = {"q": _layout(q), "k": _layout(k), "acc": _acc_layout(k)}
-    return AttnWeightsProblem(cfg, batch, attn, lse, ws, params, seq_offsets, layout)
+    return AttnWeightsProblem(cfg, batch, attn, lse, ws, dataclasses.replace(params), seq_offsets,
+                              layout)
 
 
 def run_attn_weights(prob: AttnWeightsProblem, q, k, acc, lse=None, stream=None) -> None:

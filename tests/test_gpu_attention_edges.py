@@ -165,3 +165,25 @@ def test_many_rows_of_unequal_sequences(jacap, S, G, spare):
              spare=spare, tree="tree", seed=24)
     prob, acc = run_attend(jacap, c, True, True)
     check_attend(c, prob, acc, True, True)
+
+
+def test_parameters_may_change_after_they_were_used(jacap):
+    """A problem holds the tensors whose addresses its descriptors hold, whatever becomes of
+    the parameters it was prepared with."""
+    c = Case([50, 20], 3, BF, 64, H=2, G=2, spare=5, tree="tree", seed=25)
+    p = jacap.AttentionParams(accumulate=True, live_lens=c.live, tree=c.tree,
+                              row_weight=torch.ones((2, 3), device="cuda"))
+    prob = jacap.prepare_attend(c.q, c.k, c.v, c.kd, c.vd, c.offsets, c.rows, p)
+    wp = jacap.prepare_attn_weights(c.q, c.k, c.offsets, c.rows, p)
+    live, tree, rw = p.live_lens.data_ptr(), p.tree.data_ptr(), p.row_weight.data_ptr()
+    p.live_lens = p.tree = p.row_weight = None
+    p.accumulate = False
+    for x in (prob, wp):
+        assert x.attn.live_lens == live == x.params.live_lens.data_ptr()
+        assert x.attn.tree == tree == x.params.tree.data_ptr()
+        assert x.attn.row_weight == rw == x.params.row_weight.data_ptr()
+    with pytest.raises(ValueError):   # it still accumulates
+        jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd)
+    acc = c.acc.clone()
+    jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd, acc=acc)
+    check_attend(c, prob, acc, True, True)
