@@ -605,12 +605,21 @@ def _expect_layout(prob, name: str, t: torch.Tensor) -> None:
         raise ValueError(f"{name} must have the strides the problem was prepared with")
 
 
+def _expect_device(prob, stream) -> None:
+    """The problem's device is the current one, and the stream's: what the library launches on."""
+    want = prob.ws.device.index
+    if torch.cuda.current_device() != want or \
+            (stream is not None and getattr(stream, "device_index", want) != want):
+        raise ValueError(f"the problem was prepared on cuda:{want}, not the current device or stream's")
+
+
 def _acc_layout(k: torch.Tensor):
     L, H, T, _ = k.shape
     return torch.Size((L, H, T)), (H * T, T, 1), torch.float32, k.device
 
 
 def run_attend(prob: AttendProblem, q, k, v, kd, vd, acc=None, stream=None) -> None:
+    _expect_device(prob, stream)
     for name, t in (("q", q), ("k", k), ("v", v), ("kd", kd), ("vd", vd)):
         _expect_layout(prob, name, t)
     if acc is not None or prob.params.accumulate:
@@ -649,6 +658,7 @@ def prepare_attn_weights(q, k, seq_offsets, seq_lens, params: AttentionParams) -
 
 def run_attn_weights(prob: AttnWeightsProblem, q, k, acc, lse=None, stream=None) -> None:
     """lse: the rows' log-sums if they are known (else computed into prob.lse)."""
+    _expect_device(prob, stream)
     for name, t in (("q", q), ("k", k), ("acc", acc)):
         _expect_layout(prob, name, t)
     if lse is not None:
@@ -708,6 +718,7 @@ def prepare_evict_weighted(k, v, seq_offsets, seq_lens, budget: int, protect_las
 
 
 def run_evict_weighted(prob: EvictWeightedProblem, acc, k, v, stream=None) -> None:
+    _expect_device(prob, stream)
     for name, t in (("acc", acc), ("k", k), ("v", v)):
         _expect_layout(prob, name, t)
     evict_weighted(prob.cfg, prob.batch, prob.attn, acc, k, v, prob.idx, prob.k_out, prob.v_out,
@@ -716,6 +727,7 @@ def run_evict_weighted(prob: EvictWeightedProblem, acc, k, v, stream=None) -> No
 
 def run_evict_weighted_slots(prob: EvictWeightedProblem, acc, slots, stream=None) -> None:
     """slots: int32 [B][L][H_kv][cap], cap >= max_seq_len - budget (alloc_slots); acc is updated."""
+    _expect_device(prob, stream)
     _expect_layout(prob, "acc", acc)
     units, dtype, device = prob.layout["slots"]
     if slots.shape[:-1] != units or slots.dtype != dtype or slots.device != device or \

@@ -187,3 +187,37 @@ def test_parameters_may_change_after_they_were_used(jacap):
     acc = c.acc.clone()
     jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd, acc=acc)
     check_attend(c, prob, acc, True, True)
+
+
+def test_another_device_is_refused(jacap, monkeypatch):
+    """A run with another device current, or on another device's stream, enqueues nothing."""
+    c = Case([50, 20], 3, BF, 64, H=2, G=2, seed=26)
+    p = jacap.AttentionParams(accumulate=True)
+    prob = jacap.prepare_attend(c.q, c.k, c.v, c.kd, c.vd, c.offsets, c.rows, p)
+    wp = jacap.prepare_attn_weights(c.q, c.k, c.offsets, c.rows, p)
+    ev = jacap.prepare_evict_weighted(c.k, c.v, c.offsets, c.rows, 16)
+    slots = jacap.alloc_slots(ev, c.rows)
+    acc = c.acc.clone()
+    prob.out.fill_(7.0)
+
+    class Elsewhere:
+        device_index, cuda_stream = 1, 0
+
+    def refused(stream):
+        for run in (lambda: jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd, acc=acc, stream=stream),
+                    lambda: jacap.run_attn_weights(wp, c.q, c.k, acc, stream=stream),
+                    lambda: jacap.run_evict_weighted(ev, acc, c.k, c.v, stream=stream),
+                    lambda: jacap.run_evict_weighted_slots(ev, acc, slots, stream=stream)):
+            with pytest.raises(ValueError):
+                run()
+
+    refused(Elsewhere)
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        refused(None)
+    torch.cuda.synchronize()
+    assert torch.equal(acc, c.acc) and torch.equal(prob.out, torch.full_like(prob.out, 7.0))
+    side = torch.cuda.Stream()
+    jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd, acc=acc, stream=side)
+    torch.cuda.synchronize()
+    check_attend(c, prob, acc, True, True)
