@@ -239,6 +239,12 @@ def _inputs(c, seed):
     return s
 
 
+def _restores(c):
+    """Whether a pass reads the accumulators that it writes: it adds to them, or evicts by
+    them (and marks what it evicts as empty slots)."""
+    return c["op"] == "slots" or c["decay"] > 0 and (c["acc"] or c["op"] == "weights")
+
+
 def _row_counts(s):
     return [b - a for a, b in zip(s.starts, s.starts[1:])]
 
@@ -248,7 +254,7 @@ def prepare(case, seed):
     c = s.case
     B, L, H, d = len(s.lens), c["layers"], c["kv_heads"], c["head_dim"]
     dev = "cuda"
-    if c["decay"] > 0 and s.acc is not None:
+    if _restores(c):
         s.acc0 = s.acc.clone()
     cap = max(max(_row_counts(s)), 1)
     if own:
@@ -277,8 +283,8 @@ def prepare(case, seed):
 
 def run(s):
     c = s.case
-    if c["decay"] > 0 and s.acc is not None and (c["acc"] or c["op"] == "weights"):
-        s.acc.copy_(s.acc0)   # one pass adds to the same accumulators as the last did
+    if _restores(c):
+        s.acc.copy_(s.acc0)   # one pass starts from the same accumulators as the last did
     return (_run_own if own else _run_plain)(s)
 
 
