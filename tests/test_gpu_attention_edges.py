@@ -221,3 +221,67 @@ def test_another_device_is_refused(jacap, monkeypatch):
     jacap.run_attend(prob, c.q, c.k, c.v, c.kd, c.vd, acc=acc, stream=side)
     torch.cuda.synchronize()
     check_attend(c, prob, acc, True, True)
+
+
+@pytest.mark.parametrize("S,G", [(1, 4), (9, 2), (40, 2)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_optional_outputs(jacap, S, G, accumulate):
+    """lse and acc_draft may be null: the other outputs are the same."""
+    c = Case([9000, 0, 300], S, BF, 64, H=2, G=G, holes=0.05, tree="tree" if S > 1 else None, seed=27)
+    prob, acc = run_attend(jacap, c, True, accumulate, decay=0.5)
+    want = prob.out.clone()
+    prob.out.fill_(7.0)
+    mine = c.acc.clone()
+    jacap.attend(prob.cfg, prob.batch, prob.attn, c.q, c.k, c.v, c.kd, c.vd, prob.out, None, mine, None, prob.ws)
+    assert torch.equal(prob.out, want)
+    assert torch.equal(mine, acc if accumulate else c.acc)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (F32, 64)])
+@pytest.mark.parametrize("S", [1, 20, 40])
+def test_strides_at_the_limit(jacap, dtype, d, S):
+    """K and V rows 2^24 elements apart (offsets past 2^31 bytes), and heads that share them."""
+    n, far = 37, 1 << 24
+    c = Case([n], S, dtype, d, H=2, G=2, tree="tree" if S > 1 else None, seed=28)
+    c.k, c.v = c.k[:, :1], c.v[:, :1]
+    room = [torch.empty((n - 1) * far + d, dtype=dtype, device="cuda") for _ in range(2)]
+    views = [t.as_strided((1, 2, n, d), (0, 0, far, 1)) for t in room]
+    for view, x in zip(views, (c.k, c.v)):
+        view[:, :1].copy_(x)
+    c.k, c.v = views
+    prob, acc = run_attend(jacap, c, True, True)
+    check_attend(c, prob, acc, True, True)
+    check_weights(jacap, c, True)
+
+
+@pytest.mark.parametrize("S,w", [(1, 8), (40, 300)])
+def test_accumulators_that_are_not_numbers(jacap, S, w):
+    """A NaN entry hides nothing and stays NaN; decay 0 overwrites it."""
+    c = Case([900, 31], S, BF, 64, H=2, G=4, holes=0.1, seed=29)
+    c.acc[:, :, ::7] = math.nan
+    prob, acc = run_attend(jacap, c, True, True, decay=0.5)
+    check_attend(c, prob, acc, True, True, decay=0.5)
+    prob, acc = run_attend(jacap, c, True, True, decay=0.0)
+    odd = torch.isnan(c.acc)
+    assert odd.any() and torch.isfinite(acc).all()
+    c.acc = torch.where(odd, torch.ones_like(c.acc), c.acc)
+    check_attend(c, prob, acc, True, True, decay=0.0)
+    cw = Case([900, 31], w, BF, 64, H=2, G=4, holes=0.1, seed=29)
+    cw.acc[:, :, ::7] = math.nan
+    check_weights(jacap, cw, True, decay=0.5)
+
+
+@pytest.mark.parametrize("S,G,w", [(1, 8, 64), (63, 4, 300), (20, 1, 2000)])
+def test_runs_repeat_themselves(jacap, S, G, w):
+    """The same bits from every run: joins of spans and chunks, sums of row parts."""
+    c = Case([20000, 77, 1300], S, BF, 128, H=2, G=G, holes=0.02, tree="tree" if S > 1 else None, seed=30)
+    cw = Case([20000, 77, 1300], w, BF, 128, H=2, G=G, holes=0.02, seed=30)
+    wp = jacap.prepare_attn_weights(cw.q, cw.k, cw.offsets, cw.rows, jacap.AttentionParams())
+    first = None
+    for _ in range(4):
+        prob, acc = run_attend(jacap, c, True, True)
+        weigh = cw.acc.clone()
+        jacap.run_attn_weights(wp, cw.q, cw.k, weigh)
+        got = [t.clone() for t in (prob.out, prob.lse, prob.acc_draft, acc, wp.lse, weigh)]
+        first = first or got
+        assert all(torch.equal(x, y) for x, y in zip(first, got))
