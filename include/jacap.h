@@ -359,7 +359,8 @@ jacap_status jacap_greedy(const jacap_config* cfg, const jacap_batch* batch, con
  * follows); null = all of them. A length below 0 or above the rows raises
  * JACAP_FLAG_BAD_OFFSETS, as inconsistent offsets do, and the sequence's cache
  * is taken as empty. The other sequences' results hold as long as their rows do not
- * overlap. Everything these calls read on the device may change
+ * overlap. (jacap_evict_weighted and jacap_evict_weighted_slots take such a
+ * sequence as empty too; they have no flags.) Everything these calls read on the device may change
  * between the replays of a captured graph.
  *
  * Limits (JACAP_ERR_UNSUPPORTED beyond; split the batch by layers or sequences):
@@ -376,8 +377,8 @@ jacap_status jacap_greedy(const jacap_config* cfg, const jacap_batch* batch, con
  * protect_last and the batch's out strides only by the eviction calls. Logits,
  * softmax statistics, sums over tokens and accumulators are fp32; with bf16
  * inputs the products are exact, the weights that multiply V are rounded to
- * bf16 (relative 2^-9, as out itself is), and those that are accumulated are
- * not. NaN and infinite inputs propagate as in the formulas; they raise no
+ * bf16 (by half a step at most, 2^-8 of the weight, as out itself is), and those
+ * that are accumulated are not. NaN and infinite inputs propagate as in the formulas; they raise no
  * flag. All results are deterministic. */
 typedef struct jacap_attention {
   float scale;         /* > 0, finite: 1/sqrt(d) for ordinary attention */
@@ -414,7 +415,8 @@ jacap_status jacap_evict_weighted_workspace_size(const jacap_config* cfg, const 
  *   k, v   : the cache. May be null if total_tokens = 0.
  *   kd, vd : drafted keys and values [B][L][H_kv][S][d], the dk / dv strides
  *            (multiples of 8 elements, row strides d .. 2^24).
- *   out    : [B][L][H_q][S][d], the o strides (multiples of 8), cfg->dtype.
+ *   out    : [B][L][H_q][S][d], the o strides (multiples of 8), cfg->dtype. Must
+ *            not overlap the inputs.
  *   lse    : optional float [B][L][H_q][S] (dense), natural logarithms.
  *   acc    : optional float [L][H_kv][T_total] (dense): hides the empty slots,
  *            and takes the weights when attn->accumulate = 1 (then required

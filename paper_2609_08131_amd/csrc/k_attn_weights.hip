@@ -542,15 +542,16 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_sum_kernel(Geo
 }
 
 // ---------------------------------------------------------------------------
-// Sums from the few rows of a window or a tree: all of a unit's rows lie in LDS for the whole of a workgroup's stretch of tokens. A wave takes its
-// stretch's blocks of 16 NT tokens in turn (their keys in registers, the next block's
+// Sums from the few rows of a window or a tree: all of a unit's rows lie in LDS for the
+// whole of a workgroup's stretch of tokens. A wave takes its stretch's blocks of 16 NT tokens in turn (their keys in registers, the next block's
 // requested during the last row tile) past the rows, with no barrier after the first.
 // z is carried over the blocks' ends too: a block's last logits are added, and its
 // accumulators written, as the next one's first are formed. A tile of 16 x 16 logits
 // is 96 cycles of vector instructions (an FMA, an exponential at a quarter of the rate
-// and an FMA per logit) and 64 of MFMA at d = 128. 256 rows, 32 units of 131072 tokens: 326
-// us, 430 over calls without a pause, as the clock falls; a large library product of as many
-// operations takes 240, and with the rows staged for every 256 tokens it was 530 to 590.
+// and an FMA per logit) and 64 of MFMA at d = 128: busy 59% and 40% of the cycles, 10% both
+// at once. 256 rows, 32 units of 131072 tokens: 320 us, 430 over calls without a pause, as
+// the clock falls; a large library product of as many operations takes 240, and with the
+// rows staged for every 256 tokens it was 530 to 590.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(kThreads, 2) void attn_sum_held_kernel(Geo g, Attn at, SumArgs<T> p,
