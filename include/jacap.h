@@ -475,9 +475,168 @@ jacap_status jacap_evict_weighted_slots(const jacap_config* cfg, const jacap_bat
                                         int32_t slot_cap, void* ws, size_t ws_bytes,
                                         void* stream);
 
+/* ------------------------------------------------------------------------
+ * A cache held in 8 bits, and the verification of drafted tokens.
+ *
+ * An 8-bit cache holds K and V as e4m3 values (1 sign, 4 exponent and 3 mantissa bits,
+ * largest 448, no infinities) with a scale for each block of `block` tokens of a (layer,
+ * KV head), K's and V's apart: the value is code * scale. Scales are powers of two,
+ * 2^-100 to 2^119 (of another number the mantissa is not read), so every value is exact in
+ * bfloat16, and attention over the cache is attention over those values. With a the
+ * largest finite magnitude of what a block's scale has to cover,
+ *
+ *   scale = 2^e, e the least with a <= 448 2^e, -100 <= e <= 119;
+ *   code  = x / scale rounded to the nearest e4m3 value, ties to even, at most 448 either
+ *           way; NaN for an x that is not finite.
+ *
+ * The error of a value is at most 2^-4 of it, or 2^-10 scale where that is more. A scale
+ * never falls: new tokens raise that of their block to what they need, and the codes it
+ * holds are rounded once more in units of it (exact but for the smallest ones).
+ *
+ * One serving loop: jacap_quantize after the prefill or its eviction; then for each step
+ * jacap_attend_quant over a tree of drafted tokens, jacap_verify, jacap_attn_weights_quant
+ * for the accepted rows, jacap_append_quant, and jacap_evict_weighted_slots (which reads
+ * neither K nor V) where room is wanted.
+ *
+ * Conventions as above, and: every sequence's rows begin and end at a multiple of `block`
+ * (live lengths are free); a sequence for which they do not is taken as empty and raises
+ * JACAP_FLAG_BAD_OFFSETS, as other inconsistent offsets do. total_tokens is a multiple
+ * of `block` (JACAP_ERR_INVALID_ARG). The batch's K and V strides are read by
+ * jacap_quantize only. */
+typedef struct jacap_quant {
+  int32_t block;       /* tokens per scale: 16, 32, 64 or 128 (else JACAP_ERR_UNSUPPORTED) */
+  int32_t reserved;    /* 0 */
+  /* The codes' strides, in bytes: element (l, h, t, c) at l*stride_layer + h*stride_head +
+   * t*stride_token + c. Multiples of 16; token strides d .. 2^24. Base pointers 16-byte
+   * aligned. */
+  int64_t k_stride_layer, k_stride_head, k_stride_token;
+  int64_t v_stride_layer, v_stride_head, v_stride_token;
+} jacap_quant;
+/* Scales: float [L][H_kv][total_tokens / block][2] (dense, 8-byte aligned), K's and V's of
+ * each block. */
+
+/* Writes the cache k, v (cfg->dtype, the batch's strides) into 8 bits: the codes of the
+ * tokens i < n_b of every sequence (the rows behind them keep theirs) and the scales of
+ * all blocks that the sequences own (2^-100 where a block has no token).
+ *   acc : optional float [L][H_kv][T_total] (dense): an empty slot (an entry below zero)
+ *         has no token, its codes are kept as they are.
+ * attn: live_lens is read. No workspace and no flags; num_q_heads and window are only
+ * checked. k, v must not overlap the codes. */
+jacap_status jacap_quantize(const jacap_config* cfg, const jacap_batch* batch,
+                            const jacap_attention* attn, const jacap_quant* quant, const void* k,
+                            const void* v, const float* acc, void* kq, void* vq, float* scales,
+                            void* stream);
+
+/* Writes new tokens' K and V (cfg->dtype, [B][L][H_kv][S][d] with the dk / dv strides, S =
+ * cfg->window up to 512) into the cache. Token j of sequence b, 0 <= j < count[b], is row
+ * rows[b][j] of kd and vd. It goes to position start[b] + j of the sequence, or, where slots
+ * are given, to position slots[u][start[b] + j] of each of its units u.
+ *   start  : device int32 [B]; required without slots (live_lens, commonly), null = 0 with.
+ *   count  : device int32 [B], or null: S each. Taken as 0 .. S where outside.
+ *   rows   : device int32 [B][S] (jacap_verify's path), or null: row j.
+ *   slots  : device int32 [B][L][H_kv][slot_cap] (jacap_evict_weighted_slots), or null.
+ *   acc, acc_draft : optional float [L][H_kv][T_total] and [B][L][H_kv][S] (dense): a
+ *            written token's accumulator entry becomes that of its row (0 where acc_draft
+ *            is null).
+ *   start_out : optional device int32 [B], start[b] + count[b]; may be start itself (and
+ *            must not overlap it otherwise).
+ *   status : optional device uint32 that JACAP_FLAG_BAD_OFFSETS is OR-ed into; the caller
+ *            clears it.
+ * A token whose position is not one of its sequence's rows, whose place is past the slots or
+ * whose row is not in 0 .. S-1 is not written and raises JACAP_FLAG_BAD_OFFSETS; of two
+ * tokens for one position the later is written. attn's live_lens is not read. The cache,
+ * scales and acc must not be written by others meanwhile. */
+jacap_status jacap_append_quant(const jacap_config* cfg, const jacap_batch* batch,
+                                const jacap_attention* attn, const jacap_quant* quant,
+                                const void* kd, const void* vd, const int32_t* start,
+                                const int32_t* count, const int32_t* rows, const int32_t* slots,
+                                int32_t slot_cap, void* kq, void* vq, float* scales, float* acc,
+                                const float* acc_draft, int32_t* start_out, uint32_t* status,
+                                void* stream);
+
+/* jacap_attend over an 8-bit cache; q, kd, vd and out are in cfg->dtype. With fp32 queries
+ * the logits and the weights that multiply V keep 24 bits: each is split into three bf16
+ * terms, whose products with the cache's values are exact. */
+jacap_status jacap_attend_quant_workspace_size(const jacap_config* cfg, const jacap_batch* batch,
+                                               const jacap_attention* attn, const jacap_quant* quant,
+                                               size_t* bytes);
+jacap_status jacap_attend_quant(const jacap_config* cfg, const jacap_batch* batch,
+                                const jacap_attention* attn, const jacap_quant* quant,
+                                const void* q, const void* kq, const void* vq, const float* scales,
+                                const void* kd, const void* vd, void* out, float* lse, float* acc,
+                                float* acc_draft, void* ws, size_t ws_bytes, void* stream);
+
+/* jacap_attn_weights over an 8-bit cache for rows whose log-sums are known (lse_in is
+ * required): the accepted rows of a tree, attn->causal = 0 (else JACAP_ERR_UNSUPPORTED),
+ * cfg->window up to 512. Rows of weight 0 are not read.
+ *   status : optional device uint32: JACAP_FLAG_BAD_OFFSETS, or 0. No workspace. */
+jacap_status jacap_attn_weights_quant(const jacap_config* cfg, const jacap_batch* batch,
+                                      const jacap_attention* attn, const jacap_quant* quant,
+                                      const void* q, const void* kq, const float* scales,
+                                      const float* lse_in, float* acc, uint32_t* status,
+                                      void* stream);
+
+/* Verification of drafted tokens: which rows of a chain or tree the target model accepts,
+ * and its next token, so that what a sequence receives is distributed as the target's own
+ * samples. Row 0 of a sequence is its last token, row r > 0 a drafted one, the child of row
+ * parents[b][r] < r; logits row r are the target's for the token that follows row r. With
+ * p = softmax(logits / temperature) at the current row (row 0 first), its children are
+ * tested in the order of their rows, each against its number uniform[b][r]:
+ *
+ *   no draft probabilities (children chosen without chance): x is accepted iff
+ *       u M < p(x), M = 1 - (p of the rejected siblings' tokens); after the last
+ *       rejection the weights w are p without those tokens.
+ *   draft probabilities q of the current row (its children drawn from it one by one, the
+ *       same token possibly twice): with w = p, N = 1 and C = 0 at first, x is
+ *       accepted iff u q(x) N < w(x); on a rejection C <- C + N, w <- max(p - C q, 0),
+ *       N <- sum w.
+ *
+ * An accepted child becomes the current row. Where none is left, the next token is the
+ * least x with sum_{y <= x} w(y) > uniform[b][0] sum_y w(y) (the last of positive weight
+ * where there is none; p's where rounding leaves nothing of w).
+ * temperature = 0 (greedy): the child whose token is the row's largest logit (the first of
+ * equal ones) is accepted, and the last row's largest is next; uniform and draft are not
+ * read. Sums over the vocabulary are fp64, exponentials fp32.
+ *
+ * Rows whose parent is not one of 0 .. r-1 (-1: padding) and tokens outside 0 .. vocab-1 are
+ * not tested. A current row with a NaN or +inf logit, or of only -inf (greedy: without a
+ * logit above -inf that is not NaN), or whose draft probabilities it needs are NaN, ends
+ * its sequence with next = -1 and raises JACAP_FLAG_NONFINITE. Probabilities of tokens at -inf are 0. */
+typedef struct jacap_verification {
+  int32_t num_seqs;    /* B >= 1 */
+  int32_t rows;        /* S: 1 .. 512 (else JACAP_ERR_UNSUPPORTED) */
+  int32_t vocab;       /* V >= 1, up to 2^24 (else JACAP_ERR_UNSUPPORTED) */
+  int32_t dtype;       /* of the logits: enum jacap_dtype */
+  float temperature;   /* >= 0 and finite, 1 / temperature finite */
+  int32_t reserved;    /* 0 */
+  int64_t l_stride_seq, l_stride_row;   /* logits [B][S][V]: any strides >= 0 */
+  int64_t q_stride_seq, q_stride_row;   /* draft probabilities float [B][S][V] */
+  const int32_t* parents;               /* device [B][S], or null: a chain (row r's is r - 1) */
+} jacap_verification;
+
+jacap_status jacap_verify_workspace_size(const jacap_verification* ver, size_t* bytes);
+
+/*   logits  : device, ver->dtype, aligned to it.
+ *   tokens  : device int32 [B][S] (row 0's is not read); may be null if S = 1.
+ *   uniform : device float [B][S], in [0, 1); may be null if temperature = 0.
+ *   draft   : device float [B][S][V] or null; row r the distribution that r's children were
+ *             drawn from, entries >= 0.
+ *   path    : int32 [B][S]: the accepted rows, row 0 first, -1 padding.
+ *   count   : int32 [B]: how many (row 0 among them).
+ *   next    : int32 [B]: the token behind them.
+ *   row_weight : optional float [B][S]: 1 for the accepted rows, 0 for the others
+ *             (jacap_attention.row_weight).
+ * Arrays but logits and draft are dense, all 4-byte aligned. Deterministic. The sticky
+ * flags (jacap_read_status) hold at most JACAP_FLAG_NONFINITE. */
+jacap_status jacap_verify(const jacap_verification* ver, const void* logits, const int32_t* tokens,
+                          const float* uniform, const float* draft, int32_t* path, int32_t* count,
+                          int32_t* next, float* row_weight, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* Synchronises `stream` and returns the sticky device flags (enum
  * jacap_flags, OR-ed) written by the last jacap_score / jacap_evict /
- * jacap_attend / jacap_attn_weights that used this workspace. */
+ * jacap_attend / jacap_attn_weights / jacap_attend_quant / jacap_verify that used this
+ * workspace. */
 jacap_status jacap_read_status(const void* ws, void* stream, uint32_t* flags);
 
 /* Static, human-readable name of a status code. */
@@ -489,7 +648,8 @@ const char* jacap_status_string(jacap_status s);
  *
  * While timing is on, every jacap_score / jacap_select / jacap_compact /
  * jacap_evict / jacap_greedy / jacap_attend / jacap_attn_weights /
- * jacap_evict_weighted call records a HIP event before and after each phase whose bit
+ * jacap_evict_weighted / jacap_quantize / jacap_append_quant / jacap_attend_quant /
+ * jacap_attn_weights_quant / jacap_verify call records a HIP event before and after each phase whose bit
  * (1u << phase) is set in the mask, on the stream the phase's kernels are
  * launched on; the elapsed time between the two events is that phase's GPU
  * duration. Events are created on the device that is current when the call
@@ -514,7 +674,11 @@ enum jacap_phase {
   JACAP_PHASE_ATTEND_JOIN = 14, /* ... join of the chunks, and the accumulation from kept logits */
   JACAP_PHASE_ATTN_LSE = 15,    /* jacap_attn_weights: the rows' log-sums */
   JACAP_PHASE_ATTN_SUM = 16,    /* accumulation of the weights (jacap_attend of many rows too) */
-  JACAP_NUM_PHASES = 17
+  JACAP_PHASE_QUANTIZE = 17,    /* jacap_quantize */
+  JACAP_PHASE_APPEND = 18,      /* jacap_append_quant */
+  JACAP_PHASE_VERIFY_ROWS = 19, /* jacap_verify: the rows' maxima and sums */
+  JACAP_PHASE_VERIFY = 20,      /* ... the walk over the accepted rows and the next token */
+  JACAP_NUM_PHASES = 21
 };
 
 /* Clears the accumulated times and starts recording the phases in

@@ -33,7 +33,8 @@ CFLAGS = [
 
 SOURCES = ["jacap_host.hip", "jacap_timing.hip", "k_stats.hip", "k_gram.hip", "k_factor.hip",
            "k_leverage.hip", "k_select.hip", "k_greedy.hip", "jacap_noalloc.hip",
-           "attention_host.hip", "k_attend.hip", "k_attn_weights.hip"]
+           "attention_host.hip", "k_attend.hip", "k_attn_weights.hip",
+           "quant_host.hip", "k_quant.hip", "k_attend_quant.hip", "verify_host.hip", "k_verify.hip"]
 
 
 def _compile(src: str, verbose: bool) -> str:

@@ -54,9 +54,11 @@ struct Attn {
   float decay;
   int accumulate, causal;
   int R;           // rows per KV head: G * window, row r = head r / window, position r % window
+  int tree_words;  // 32-bit words of a row of `tree`
+  int row_mask;    // an 8-bit cache's tokens per scale less 1, else 0: sequences begin and end at
+                   // multiples
   const float* row_weight;
-  const uint32_t* tree;  // 32-bit words, little end first
-  int tree_words;        // ... per row
+  const uint32_t* tree;  // little end first
   int64_t dks, dkl, dkh, dkr, dvs, dvl, dvh, dvr, os, ol, oh, op;
 };
 
@@ -140,13 +142,25 @@ __device__ __forceinline__ const T* unit_queries(const Geo& g, const Unit& un, c
   return q + un.b * g.qss + un.l * g.qsl + (int64_t)un.h * g.G * g.qsh;
 }
 
+// Whether sequence b's rows are whole blocks of an 8-bit cache; one of which they are not
+// is taken as empty.
+__device__ __forceinline__ bool whole_blocks(const Geo& g, const Attn& at, int b) {
+  return at.row_mask == 0 || ((g.seq_off[b] | g.seq_off[b + 1]) & at.row_mask) == 0;
+}
+// live_unit of either cache.
+__device__ __forceinline__ Unit attention_unit(const Geo& g, const Attn& at, int u) {
+  Unit r = live_unit(g, u);
+  if (!whole_blocks(g, at, r.b)) r.n = 0;
+  return r;
+}
+
 // The status word: bad offsets or lengths of any sequence. Called by every
 // thread of one workgroup.
-__device__ __forceinline__ void write_status(const Geo& g, uint32_t* status) {
+__device__ __forceinline__ void write_status(const Geo& g, const Attn& at, uint32_t* status) {
   int bad = 0;
   for (int b = threadIdx.x; b < g.B; b += kThreads) {
     const int32_t a = g.seq_off[b], e = g.seq_off[b + 1];
-    const bool ok = offsets_ok(g, a, e);
+    const bool ok = offsets_ok(g, a, e) && whole_blocks(g, at, b);
     bad |= !ok || !live_ok(g, b, e - a);
   }
   bad = __syncthreads_or(bad);
@@ -208,8 +222,19 @@ hipError_t launch_attend(const AttnLaunch& A, const AttendSpace& w, const void* 
 bool attend_joins(const AttnLaunch& A, const AttendSpace& w);
 hipError_t launch_attend_join(const AttnLaunch& A, const AttendSpace& w, void* out, float* lse,
                               float* acc, float* acc_draft);
+// The same for spans cut in groups of another number of tokens.
+hipError_t launch_attend_join_groups(const AttnLaunch& A, const AttendSpace& w, int group, void* out,
+                                     float* lse, float* acc, float* acc_draft);
 hipError_t launch_attn_lse(const AttnLaunch& A, const WeightsSpace& w, const void* q, const void* k,
                            const float* acc, float* lse);
+// What the entry points of the attention share (attention_host.hip): the checks of the
+// descriptors, and the workspace of jacap_attend (sum: the cut of the accumulation's own
+// pass, for more rows than keep their logits).
+jacap_status check_attention(const jacap_config* cfg, const jacap_batch* batch, const jacap_attention* at,
+                             void* stream, AttnLaunch* A);
+jacap_status check_attend(const jacap_config* cfg, const jacap_batch* batch, const jacap_attention* at,
+                          void* stream, AttnLaunch* A);
+jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, WeightsSpace* sum);
 // Adds the rows' weights, given their log-sums, to acc; status may be null.
 hipError_t launch_attn_sum(const AttnLaunch& A, const WeightsSpace& w, const void* q, const void* k,
                            const float* lse, float* acc, uint32_t* status);

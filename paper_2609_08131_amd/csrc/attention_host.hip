@@ -26,9 +26,11 @@ bool optional_ok(const void* p, uintptr_t align) { return !p || aligned(p, align
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
+}  // namespace
+
 // The descriptor and what every call shares. ws = null: no workspace is checked.
-jacap_status check(const jacap_config* cfg, const jacap_batch* batch, const jacap_attention* at,
-                   void* stream, AttnLaunch* A) {
+jacap_status jacap::check_attention(const jacap_config* cfg, const jacap_batch* batch,
+                                    const jacap_attention* at, void* stream, AttnLaunch* A) {
   if (!batch || !at) return JACAP_ERR_INVALID_ARG;
   // No sequence is longer than all of them, whatever length the caller declares: what is cut
   // and counted below (in 32 bits, up to a chunk past the end) follows the shorter.
@@ -58,9 +60,9 @@ jacap_status check(const jacap_config* cfg, const jacap_batch* batch, const jaca
   return JACAP_OK;
 }
 
-jacap_status check_attend(const jacap_config* cfg, const jacap_batch* batch,
-                          const jacap_attention* at, void* stream, AttnLaunch* A) {
-  const jacap_status s = check(cfg, batch, at, stream, A);
+jacap_status jacap::check_attend(const jacap_config* cfg, const jacap_batch* batch,
+                                 const jacap_attention* at, void* stream, AttnLaunch* A) {
+  const jacap_status s = check_attention(cfg, batch, at, stream, A);
   if (s != JACAP_OK) return s;
   if (cfg->window > kMaxDraft) return JACAP_ERR_UNSUPPORTED;
   const int64_t st[] = {at->dk_stride_seq, at->dk_stride_layer, at->dk_stride_head,
@@ -80,6 +82,8 @@ jacap_status check_attend(const jacap_config* cfg, const jacap_batch* batch,
   a.os = at->o_stride_seq; a.ol = at->o_stride_layer; a.oh = at->o_stride_head; a.op = at->o_stride_pos;
   return JACAP_OK;
 }
+
+namespace {
 
 // How the passes over rows and tokens of the weights are cut; `o` the
 // workspace's size so far. The chunks of the log-sums are one round of the chip (fp32
@@ -144,9 +148,9 @@ jacap_status layout_weights(const AttnLaunch& A, bool bf16, WeightsSpace* w) {
   return sum_grid_ok(g, *w) ? JACAP_OK : JACAP_ERR_UNSUPPORTED;
 }
 
-// sum: the accumulation's own cut, for accumulating from more rows than keep
-// their logits.
-jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, WeightsSpace* sum) {
+}  // namespace
+
+jacap_status jacap::layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, WeightsSpace* sum) {
   const Geo& g = A.base.geo;
   const int64_t UR = (int64_t)g.U * A.at.R, LHT = (int64_t)g.L * g.H * g.T;
   if (UR > kMaxGrid) return JACAP_ERR_UNSUPPORTED;
@@ -200,6 +204,8 @@ jacap_status layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, Weigh
     return JACAP_ERR_UNSUPPORTED;
   return JACAP_OK;
 }
+
+namespace {
 
 bool is_bf16(const jacap_config* c) { return c->dtype == JACAP_DTYPE_BF16; }
 
@@ -274,7 +280,7 @@ jacap_status jacap_attn_weights_workspace_size(const jacap_config* cfg, const ja
                                                const jacap_attention* attn, size_t* bytes) {
   if (!bytes) return JACAP_ERR_INVALID_ARG;
   AttnLaunch A;
-  jacap_status s = check(cfg, batch, attn, nullptr, &A);
+  jacap_status s = check_attention(cfg, batch, attn, nullptr, &A);
   if (s != JACAP_OK) return s;
   WeightsSpace w;
   s = layout_weights(A, is_bf16(cfg), &w);
@@ -288,7 +294,7 @@ jacap_status jacap_attn_weights(const jacap_config* cfg, const jacap_batch* batc
                                 const float* lse_in, float* lse_out, float* acc, void* ws,
                                 size_t ws_bytes, void* stream) {
   AttnLaunch A;
-  jacap_status s = check(cfg, batch, attn, stream, &A);
+  jacap_status s = check_attention(cfg, batch, attn, stream, &A);
   if (s != JACAP_OK) return s;
   WeightsSpace w;
   s = layout_weights(A, is_bf16(cfg), &w);
@@ -314,7 +320,7 @@ jacap_status jacap_evict_weighted_workspace_size(const jacap_config* cfg, const 
                                                  const jacap_attention* attn, size_t* bytes) {
   if (!bytes) return JACAP_ERR_INVALID_ARG;
   AttnLaunch A;
-  const jacap_status s = check(cfg, batch, attn, nullptr, &A);
+  const jacap_status s = check_attention(cfg, batch, attn, nullptr, &A);
   if (s != JACAP_OK) return s;
   *bytes = kept_bytes(cfg, A.base.geo);
   return JACAP_OK;
@@ -325,7 +331,7 @@ jacap_status jacap_evict_weighted(const jacap_config* cfg, const jacap_batch* ba
                                   const void* v, int32_t* idx, void* k_out, void* v_out,
                                   float* acc_out, void* stream) {
   AttnLaunch A;
-  const jacap_status s = check(cfg, batch, attn, stream, &A);
+  const jacap_status s = check_attention(cfg, batch, attn, stream, &A);
   if (s != JACAP_OK) return s;
   if (attn->a_stride_seq < 0 || attn->a_stride_layer < 0 || attn->a_stride_head < 0)
     return JACAP_ERR_INVALID_ARG;
@@ -350,7 +356,7 @@ jacap_status jacap_evict_weighted_slots(const jacap_config* cfg, const jacap_bat
                                         int32_t slot_cap, void* ws, size_t ws_bytes,
                                         void* stream) {
   AttnLaunch A;
-  jacap_status s = check(cfg, batch, attn, stream, &A);
+  jacap_status s = check_attention(cfg, batch, attn, stream, &A);
   if (s != JACAP_OK) return s;
   s = take_workspace(ws, ws_bytes, kept_bytes(cfg, A.base.geo), &A.base);
   if (s != JACAP_OK) return s;

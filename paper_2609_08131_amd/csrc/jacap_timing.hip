@@ -100,7 +100,7 @@ const char* jacap_phase_name(int32_t phase) {
                                                  "gram_reduce", "factor", "refine", "leverage",
                                                  "select", "compact", "greedy_init",
                                                  "greedy", "attend", "attend_join", "attn_lse",
-                                                 "attn_sum"};
+                                                 "attn_sum", "quantize", "append", "verify_rows", "verify"};
   if (phase < 0 || phase >= JACAP_NUM_PHASES) return "unknown";
   return names[phase];
 }

@@ -538,7 +538,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_sum_kernel(Geo
       }
     }
   }
-  if (blockIdx.x == 0 && p.status) write_status(g, p.status);
+  if (blockIdx.x == 0 && p.status) write_status(g, at, p.status);
 }
 
 // ---------------------------------------------------------------------------
@@ -690,7 +690,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_sum_held_kernel(Geo g, Attn 
       }
     }
   }
-  if (blockIdx.x == 0 && p.status) write_status(g, p.status);
+  if (blockIdx.x == 0 && p.status) write_status(g, at, p.status);
 }
 
 // The row parts' sums, in order.

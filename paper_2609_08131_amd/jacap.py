@@ -92,6 +92,26 @@ class Attention(ctypes.Structure):
     ]
 
 
+class Quant(ctypes.Structure):
+    _fields_ = [
+        ("block", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("k_stride_layer", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+        ("k_stride_token", ctypes.c_int64),
+        ("v_stride_layer", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
+        ("v_stride_token", ctypes.c_int64),
+    ]
+
+
+class Verification(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("l_stride_seq", ctypes.c_int64), ("l_stride_row", ctypes.c_int64),
+        ("q_stride_seq", ctypes.c_int64), ("q_stride_row", ctypes.c_int64),
+        ("parents", ctypes.c_void_p),
+    ]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -99,7 +119,8 @@ def _load() -> ctypes.CDLL:
             "`python -m paper_2609_08131_amd.build` (there is no CPU fallback)")
     lib = ctypes.CDLL(LIB_PATH)
     P, C, B = ctypes.c_void_p, ctypes.POINTER(Config), ctypes.POINTER(Batch)
-    A = ctypes.POINTER(Attention)
+    A, Q = ctypes.POINTER(Attention), ctypes.POINTER(Quant)
+    V, I = ctypes.POINTER(Verification), ctypes.c_int32
     sz = ctypes.c_size_t
     sigs = {
         "jacap_workspace_size": [C, B, ctypes.POINTER(sz)],
@@ -122,6 +143,13 @@ def _load() -> ctypes.CDLL:
         "jacap_evict_weighted_workspace_size": [C, B, A, ctypes.POINTER(sz)],
         "jacap_evict_weighted": [C, B, A, P, P, P, P, P, P, P, P],
         "jacap_evict_weighted_slots": [C, B, A, P, P, ctypes.c_int32, P, sz, P],
+        "jacap_quantize": [C, B, A, Q, P, P, P, P, P, P, P],
+        "jacap_append_quant": [C, B, A, Q, P, P, P, P, P, P, I, P, P, P, P, P, P, P, P],
+        "jacap_attend_quant_workspace_size": [C, B, A, Q, ctypes.POINTER(sz)],
+        "jacap_attend_quant": [C, B, A, Q, P, P, P, P, P, P, P, P, P, P, P, sz, P],
+        "jacap_attn_weights_quant": [C, B, A, Q, P, P, P, P, P, P, P],
+        "jacap_verify_workspace_size": [V, ctypes.POINTER(sz)],
+        "jacap_verify": [V, P, P, P, P, P, P, P, P, P, sz, P],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -146,8 +174,10 @@ EXPORTED = ("jacap_workspace_size", "jacap_score", "jacap_score_from_stats", "ja
             "jacap_select_evicted", "jacap_evict_slots", "jacap_evict_noalloc",
             "jacap_attend_workspace_size", "jacap_attend", "jacap_attn_weights_workspace_size",
             "jacap_attn_weights", "jacap_evict_weighted_workspace_size", "jacap_evict_weighted",
-            "jacap_evict_weighted_slots")
-NUM_PHASES = 17   # enum jacap_phase
+            "jacap_evict_weighted_slots", "jacap_quantize", "jacap_append_quant",
+            "jacap_attend_quant_workspace_size", "jacap_attend_quant", "jacap_attn_weights_quant",
+            "jacap_verify_workspace_size", "jacap_verify")
+NUM_PHASES = 21   # enum jacap_phase
 
 
 def status_string(code: int) -> str:
@@ -391,6 +421,55 @@ def evict_weighted_slots(cfg, batch, attn, acc, slots, ws, stream=None) -> None:
         int(slots.shape[-1]), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)))
 
 
+def quantize(cfg, batch, attn, quant, k, v, acc, kq, vq, scales, stream=None) -> None:
+    _check("jacap_quantize", _lib.jacap_quantize(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(quant), _ptr(k), _ptr(v),
+        _ptr(acc), _ptr(kq), _ptr(vq), _ptr(scales), _stream(stream)))
+
+
+def append_quant(cfg, batch, attn, quant, kd, vd, start, count, rows, slots, kq, vq, scales, acc, acc_draft,
+                 start_out, status, stream=None) -> None:
+    """slots: int32 [B][L][H][slot_cap] (the last dimension is the capacity), or None."""
+    _check("jacap_append_quant", _lib.jacap_append_quant(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(quant), _ptr(kd), _ptr(vd),
+        _ptr(start), _ptr(count), _ptr(rows), _ptr(slots), int(slots.shape[-1]) if slots is not None else 0,
+        _ptr(kq), _ptr(vq), _ptr(scales), _ptr(acc), _ptr(acc_draft), _ptr(start_out), _ptr(status),
+        _stream(stream)))
+
+
+def attend_quant_workspace_size(cfg: Config, batch: Batch, attn: Attention, quant: Quant) -> int:
+    n = ctypes.c_size_t(0)
+    _check("jacap_attend_quant_workspace_size", _lib.jacap_attend_quant_workspace_size(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(quant), ctypes.byref(n)))
+    return int(n.value)
+
+
+def attend_quant(cfg, batch, attn, quant, q, kq, vq, scales, kd, vd, out, lse, acc, acc_draft, ws,
+                 stream=None) -> None:
+    _check("jacap_attend_quant", _lib.jacap_attend_quant(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(quant), _ptr(q), _ptr(kq),
+        _ptr(vq), _ptr(scales), _ptr(kd), _ptr(vd), _ptr(out), _ptr(lse), _ptr(acc), _ptr(acc_draft), _ptr(ws),
+        ws.numel() if ws is not None else 0, _stream(stream)))
+
+
+def attn_weights_quant(cfg, batch, attn, quant, q, kq, scales, lse_in, acc, status=None, stream=None) -> None:
+    _check("jacap_attn_weights_quant", _lib.jacap_attn_weights_quant(
+        ctypes.byref(cfg), ctypes.byref(batch), ctypes.byref(attn), ctypes.byref(quant), _ptr(q), _ptr(kq),
+        _ptr(scales), _ptr(lse_in), _ptr(acc), _ptr(status), _stream(stream)))
+
+
+def verify_workspace_size(ver: Verification) -> int:
+    n = ctypes.c_size_t(0)
+    _check("jacap_verify_workspace_size", _lib.jacap_verify_workspace_size(ctypes.byref(ver), ctypes.byref(n)))
+    return int(n.value)
+
+
+def verify(ver, logits, tokens, uniform, draft, path, count, next_token, row_weight, ws, stream=None) -> None:
+    _check("jacap_verify", _lib.jacap_verify(
+        ctypes.byref(ver), _ptr(logits), _ptr(tokens), _ptr(uniform), _ptr(draft), _ptr(path), _ptr(count),
+        _ptr(next_token), _ptr(row_weight), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)))
+
+
 # ---------------------------------------------------------------------------
 # Convenience: allocate outputs and run the whole path on torch tensors
 # ---------------------------------------------------------------------------
@@ -607,7 +686,11 @@ def _expect_layout(prob, name: str, t: torch.Tensor) -> None:
 
 def _expect_device(prob, stream) -> None:
     """The problem's device is the current one, and the stream's: what the library launches on."""
-    want = prob.ws.device.index
+    _expect_current(prob.ws.device, stream)
+
+
+def _expect_current(device, stream) -> None:
+    want = device.index
     if torch.cuda.current_device() != want or \
             (stream is not None and getattr(stream, "device_index", want) != want):
         raise ValueError(f"the problem was prepared on cuda:{want}, not the current device or stream's")
@@ -734,6 +817,340 @@ def run_evict_weighted_slots(prob: EvictWeightedProblem, acc, slots, stream=None
             not slots.is_contiguous():
         _expect("slots", slots, (*units, slots.shape[-1] if slots.dim() else 0), dtype, device)
     evict_weighted_slots(prob.cfg, prob.batch, prob.attn, acc, slots, prob.ws, stream)
+
+
+# ---------------------------------------------------------------------------
+# A cache held in 8 bits, and the verification of drafted tokens
+# ---------------------------------------------------------------------------
+
+@dataclasses.dataclass
+class QuantCache:
+    """K and V as e4m3 codes with a power-of-two scale for each block of tokens of a (layer,
+    KV head): the values are codes times scales (see jacap_quant in include/jacap.h)."""
+
+    k: torch.Tensor         # float8_e4m3fn [L][H_kv][T_total][d] (views too, d contiguous)
+    v: torch.Tensor
+    scales: torch.Tensor    # float32 [L][H_kv][T_total / block][2]: K's, V's
+    block: int              # 16, 32, 64 or 128; sequences begin at its multiples
+
+
+def alloc_quant_cache(layers: int, kv_heads: int, tokens: int, head_dim: int, block: int = 32,
+                      device="cuda") -> QuantCache:
+    """An 8-bit cache without tokens: codes of 0, the least scale."""
+    if block <= 0 or tokens % block != 0:
+        raise ValueError(f"tokens must be a multiple of the block, {block}")
+    k = torch.zeros((layers, kv_heads, tokens, head_dim), dtype=torch.float8_e4m3fn, device=device)
+    scales = torch.full((layers, kv_heads, tokens // block, 2), 2.0 ** -100, device=device)
+    return QuantCache(k, torch.zeros_like(k), scales, block)
+
+
+def _quant_checks(seq_offsets, seq_lens, cache: QuantCache) -> Quant:
+    k, v = cache.k, cache.v
+    if k.dim() != 4 or k.dtype != torch.float8_e4m3fn:
+        raise ValueError("the cache's k must be float8_e4m3fn [L][H_kv][T_total][d]")
+    if not k.is_cuda or k.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {k.device}, not on the current device")
+    L, H, T, d = k.shape
+    bk = int(cache.block)
+    if bk not in (16, 32, 64, 128):
+        raise ValueError("the cache's block must be 16, 32, 64 or 128 tokens")
+    if sum(int(n) for n in seq_lens) != T or any(int(n) % bk for n in seq_lens):
+        raise ValueError(f"seq_lens must be multiples of the block, {bk}, that sum to the cache's {T} rows")
+    _expect("k", k, k.shape, k.dtype, k.device, dense=False)
+    _expect("v", v, k.shape, k.dtype, k.device, dense=False)
+    _expect("scales", cache.scales, (L, H, T // bk, 2), torch.float32, k.device)
+    _expect("seq_offsets", seq_offsets, (len(seq_lens) + 1,), torch.int32, k.device)
+    return Quant(bk, 0, *k.stride()[:3], *v.stride()[:3])
+
+
+def _quant_config(cache: QuantCache, dtype, q_heads: int, rows: int) -> Config:
+    if dtype not in _DTYPE_CODE:
+        raise ValueError("tensors beside the 8-bit cache must be float32 or bfloat16")
+    L, H, _, d = cache.k.shape
+    p = Params(budget_k=0)
+    return Config(L, H, q_heads, d, rows, 0, p.temperature, p.ridge, p.cov_mode, _DTYPE_CODE[dtype],
+                  RIDGE_SCALAR, p.gqa_mode, 0)
+
+
+def _cache_layout(cache: QuantCache) -> dict:
+    return {"cache.k": _layout(cache.k), "cache.v": _layout(cache.v), "scales": _layout(cache.scales),
+            "acc": _acc_layout(cache.k)}
+
+
+def _expect_cache(prob, cache: QuantCache) -> None:
+    _expect_layout(prob, "cache.k", cache.k)
+    _expect_layout(prob, "cache.v", cache.v)
+    _expect_layout(prob, "scales", cache.scales)
+
+
+@dataclasses.dataclass
+class QuantizeProblem:
+    """Descriptors of jacap_quantize for one batch."""
+
+    cfg: Config
+    batch: Batch
+    attn: Attention
+    quant: Quant
+    params: AttentionParams
+    seq_offsets: torch.Tensor
+    layout: dict
+
+
+def prepare_quantize(k, v, cache: QuantCache, seq_offsets, seq_lens, live_lens=None) -> QuantizeProblem:
+    """seq_lens: the rows each sequence owns, of both caches (multiples of the block; their
+    current lengths where live_lens gives none)."""
+    quant = _quant_checks(seq_offsets, seq_lens, cache)
+    _cache_checks(seq_offsets, seq_lens, k, ("v", v, k.shape))
+    L, H, T, d = cache.k.shape
+    if tuple(k.shape) != (L, H, T, d):
+        raise ValueError(f"k must have the 8-bit cache's shape {(L, H, T, d)}")
+    params = AttentionParams(live_lens=live_lens)
+    cfg = _quant_config(cache, k.dtype, H, 1)
+    batch = make_batch(seq_offsets, seq_lens, k.new_empty((len(seq_lens), L, H, 1, d)), k, v)
+    attn = _attention(params, len(seq_lens), 1, d, k.device)
+    layout = {"k": _layout(k), "v": _layout(v), **_cache_layout(cache)}
+    return QuantizeProblem(cfg, batch, attn, quant, params, seq_offsets, layout)
+
+
+def run_quantize(prob: QuantizeProblem, k, v, cache: QuantCache, acc=None, stream=None) -> None:
+    """acc: the accumulators, whose empty slots are left out (None: there are none)."""
+    _expect_current(prob.seq_offsets.device, stream)
+    for name, t in (("k", k), ("v", v)):
+        _expect_layout(prob, name, t)
+    _expect_cache(prob, cache)
+    if acc is not None:
+        _expect_layout(prob, "acc", acc)
+    quantize(prob.cfg, prob.batch, prob.attn, prob.quant, k, v, acc, cache.k, cache.v, cache.scales, stream)
+
+
+@dataclasses.dataclass
+class AppendProblem:
+    """Descriptors and outputs of jacap_append_quant for one batch."""
+
+    cfg: Config
+    batch: Batch
+    attn: Attention
+    quant: Quant
+    start_out: torch.Tensor     # int32 [B]: start + count of the last run
+    status: torch.Tensor        # int32 [1]: flags of all runs, cleared by the caller
+    seq_offsets: torch.Tensor
+    layout: dict
+
+
+def prepare_append_quant(kd, vd, cache: QuantCache, seq_offsets, seq_lens) -> AppendProblem:
+    """kd, vd [B][L][H_kv][S][d]: the tokens that may be appended; seq_lens as prepare_quantize."""
+    quant = _quant_checks(seq_offsets, seq_lens, cache)
+    L, H, _, d = cache.k.shape
+    B, dev = len(seq_lens), cache.k.device
+    if kd.dim() != 5:
+        raise ValueError("kd must be [B][L][H_kv][S][d]")
+    S = kd.shape[3]
+    for name, t in (("kd", kd), ("vd", vd)):
+        _expect(name, t, (B, L, H, S, d), kd.dtype, dev, dense=False)
+    cfg = _quant_config(cache, kd.dtype, H, S)
+    batch = make_batch(seq_offsets, seq_lens, kd.new_empty((B, L, H, S, d)), cache.k, cache.v)
+    attn = _attention(AttentionParams(), B, S, d, dev)
+    _strides(attn, "dk", kd)
+    _strides(attn, "dv", vd)
+    attn.o_stride_pos = d
+    layout = {"kd": _layout(kd), "vd": _layout(vd), **_cache_layout(cache)}
+    return AppendProblem(cfg, batch, attn, quant, torch.empty((B,), dtype=torch.int32, device=dev),
+                         torch.zeros((1,), dtype=torch.int32, device=dev), seq_offsets, layout)
+
+
+def run_append_quant(prob: AppendProblem, kd, vd, cache: QuantCache, start=None, rows=None, count=None,
+                     slots=None, acc=None, acc_draft=None, start_out=None, stream=None) -> None:
+    """start int32 [B] (required without slots): the first token's position, or its place in
+    slots int32 [B][L][H_kv][cap]; rows int32 [B][S], count int32 [B]: which rows of kd and
+    vd (all where None); start_out: where start + count goes (None: prob.start_out; start
+    itself to move on in place)."""
+    dev = prob.seq_offsets.device
+    _expect_current(dev, stream)
+    for name, t in (("kd", kd), ("vd", vd)):
+        _expect_layout(prob, name, t)
+    _expect_cache(prob, cache)
+    B, L, H, S = kd.shape[:4]
+    if start is None and slots is None:
+        raise ValueError("start is missing")
+    start_out = prob.start_out if start_out is None else start_out
+    for name, t, shape in (("start", start, (B,)), ("rows", rows, (B, S)), ("count", count, (B,)),
+                           ("start_out", start_out, (B,))):
+        if t is not None:
+            _expect(name, t, shape, torch.int32, dev)
+    if slots is not None:
+        _expect("slots", slots, (B, L, H, slots.shape[-1] if slots.dim() else 0), torch.int32, dev)
+    if acc is not None:
+        _expect_layout(prob, "acc", acc)
+    if acc_draft is not None:
+        _expect("acc_draft", acc_draft, (B, L, H, S), torch.float32, dev)
+    append_quant(prob.cfg, prob.batch, prob.attn, prob.quant, kd, vd, start, count, rows, slots, cache.k,
+                 cache.v, cache.scales, acc, acc_draft, start_out, prob.status, stream)
+
+
+@dataclasses.dataclass
+class AttendQuantProblem:
+    """Descriptors, outputs and workspace of jacap_attend_quant for one batch (as AttendProblem)."""
+
+    cfg: Config
+    batch: Batch
+    attn: Attention
+    quant: Quant
+    out: torch.Tensor                     # [B][L][H_q][S][d]
+    lse: torch.Tensor                     # float32 [B][L][H_q][S]
+    acc_draft: Optional[torch.Tensor]     # float32 [B][L][H_kv][S], with accumulate
+    ws: torch.Tensor
+    params: AttentionParams
+    seq_offsets: torch.Tensor
+    layout: dict
+
+
+def prepare_attend_quant(q, cache: QuantCache, kd, vd, seq_offsets, seq_lens,
+                         params: AttentionParams) -> AttendQuantProblem:
+    """prepare_attend over an 8-bit cache; seq_lens as prepare_quantize."""
+    quant = _quant_checks(seq_offsets, seq_lens, cache)
+    L, H, _, d = cache.k.shape
+    B, dev = len(seq_lens), cache.k.device
+    if q.dim() != 5:
+        raise ValueError("q must be [B][L][H_q][S][d]")
+    Hq, S = q.shape[2:4]
+    for name, t, heads in (("q", q, Hq), ("kd", kd, H), ("vd", vd, H)):
+        _expect(name, t, (B, L, heads, S, d), q.dtype, dev, dense=False)
+    cfg = _quant_config(cache, q.dtype, Hq, S)
+    batch = make_batch(seq_offsets, seq_lens, q, cache.k, cache.v)
+    attn = _attention(params, B, S, d, dev)
+    out = torch.empty((B, L, Hq, S, d), dtype=q.dtype, device=dev)
+    _strides(attn, "dk", kd)
+    _strides(attn, "dv", vd)
+    attn.o_stride_seq, attn.o_stride_layer, attn.o_stride_head, attn.o_stride_pos = out.stride()[:4]
+    ws = _workspace(attend_quant_workspace_size(cfg, batch, attn, quant), dev)
+    lse = torch.empty((B, L, Hq, S), dtype=torch.float32, device=dev)
+    acc_draft = torch.empty((B, L, H, S), dtype=torch.float32, device=dev) if params.accumulate else None
+    layout = {"q": _layout(q), "kd": _layout(kd), "vd": _layout(vd), **_cache_layout(cache)}
+    return AttendQuantProblem(cfg, batch, attn, quant, out, lse, acc_draft, ws, dataclasses.replace(params),
+                              seq_offsets, layout)
+
+
+def run_attend_quant(prob: AttendQuantProblem, q, cache: QuantCache, kd, vd, acc=None, stream=None) -> None:
+    _expect_device(prob, stream)
+    for name, t in (("q", q), ("kd", kd), ("vd", vd)):
+        _expect_layout(prob, name, t)
+    _expect_cache(prob, cache)
+    if acc is not None or prob.params.accumulate:
+        _expect_layout(prob, "acc", acc)
+    attend_quant(prob.cfg, prob.batch, prob.attn, prob.quant, q, cache.k, cache.v, cache.scales, kd, vd,
+                 prob.out, prob.lse, acc, prob.acc_draft, prob.ws, stream)
+
+
+@dataclasses.dataclass
+class AttnWeightsQuantProblem:
+    """Descriptors of jacap_attn_weights_quant for one batch."""
+
+    cfg: Config
+    batch: Batch
+    attn: Attention
+    quant: Quant
+    status: torch.Tensor    # int32 [1]: the last run's flags
+    params: AttentionParams
+    seq_offsets: torch.Tensor
+    layout: dict
+
+
+def prepare_attn_weights_quant(q, cache: QuantCache, seq_offsets, seq_lens,
+                               params: AttentionParams) -> AttnWeightsQuantProblem:
+    """q [B][L][H_q][w][d]; seq_lens as prepare_quantize; params.causal is not read: every row
+    sees every token."""
+    quant = _quant_checks(seq_offsets, seq_lens, cache)
+    L, H, _, d = cache.k.shape
+    B, dev = len(seq_lens), cache.k.device
+    if q.dim() != 5:
+        raise ValueError("q must be [B][L][H_q][w][d]")
+    Hq, w = q.shape[2:4]
+    _expect("q", q, (B, L, Hq, w, d), q.dtype, dev, dense=False)
+    cfg = _quant_config(cache, q.dtype, Hq, w)
+    batch = make_batch(seq_offsets, seq_lens, q, cache.k, cache.v)
+    attn = _attention(params, B, w, d, dev)
+    attn.causal = 0
+    layout = {"q": _layout(q), **_cache_layout(cache),
+              "lse": _layout(torch.empty((B, L, Hq, w), device=dev))}
+    return AttnWeightsQuantProblem(cfg, batch, attn, quant, torch.zeros((1,), dtype=torch.int32, device=dev),
+                                   dataclasses.replace(params), seq_offsets, layout)
+
+
+def run_attn_weights_quant(prob: AttnWeightsQuantProblem, q, cache: QuantCache, acc, lse, stream=None) -> None:
+    """lse float32 [B][L][H_q][w]: the rows' log-sums, as run_attend_quant left them."""
+    _expect_current(prob.seq_offsets.device, stream)
+    _expect_layout(prob, "q", q)
+    _expect_cache(prob, cache)
+    _expect_layout(prob, "acc", acc)
+    _expect_layout(prob, "lse", lse)
+    attn_weights_quant(prob.cfg, prob.batch, prob.attn, prob.quant, q, cache.k, cache.scales, lse, acc,
+                       prob.status, stream)
+
+
+@dataclasses.dataclass
+class VerifyParams:
+    """Parameters of verify (see jacap_verification in include/jacap.h)."""
+
+    temperature: float = 1.0                    # 0: greedy
+    parents: Optional[torch.Tensor] = None      # device int32 [B][S]; None: a chain
+
+
+@dataclasses.dataclass
+class VerifyProblem:
+    """Descriptor, outputs and workspace of jacap_verify for one batch."""
+
+    ver: Verification
+    path: torch.Tensor          # int32 [B][S]: accepted rows, -1 padding
+    count: torch.Tensor         # int32 [B]: how many, row 0 among them
+    next: torch.Tensor          # int32 [B]: the token behind them
+    row_weight: torch.Tensor    # float32 [B][S]: 1 for the accepted rows (attn_weights)
+    ws: torch.Tensor
+    params: VerifyParams
+    layout: dict
+
+
+def prepare_verify(logits, params: VerifyParams, draft=None) -> VerifyProblem:
+    """logits [B][S][V], float32 or bfloat16; draft: float32 [B][S][V], the draft model's
+    probabilities, where the drafted tokens were drawn from them (the vocabulary contiguous
+    in both)."""
+    if logits.dim() != 3 or logits.dtype not in _DTYPE_CODE:
+        raise ValueError("logits must be float32 or bfloat16 [B][S][V]")
+    if not logits.is_cuda or logits.device.index != torch.cuda.current_device():
+        raise ValueError(f"logits are on {logits.device}, not on the current device")
+    B, S, V = logits.shape
+    dev = logits.device
+    layout = {"draft": None, "uniform": (B, S), "tokens": (B, S)}
+    for name, t, dtype in (("logits", logits, logits.dtype), ("draft", draft, torch.float32)):
+        if t is None:
+            continue
+        if tuple(t.shape) != (B, S, V) or t.dtype != dtype or t.device != dev or (V > 1 and t.stride(2) != 1):
+            raise ValueError(f"{name} must be a {dtype} [B][S][V] tensor on {dev}, the vocabulary contiguous")
+        layout[name] = _layout(t)
+    ver = Verification(B, S, V, _DTYPE_CODE[logits.dtype], float(params.temperature), 0,
+                       *logits.stride()[:2], *(draft.stride()[:2] if draft is not None else (0, 0)))
+    if params.parents is not None:
+        _expect("parents", params.parents, (B, S), torch.int32, dev)
+        ver.parents = params.parents.data_ptr()
+    ints = [torch.empty(shape, dtype=torch.int32, device=dev) for shape in ((B, S), (B,), (B,))]
+    ws = _workspace(verify_workspace_size(ver), dev)
+    return VerifyProblem(ver, *ints, torch.empty((B, S), device=dev), ws, dataclasses.replace(params), layout)
+
+
+def run_verify(prob: VerifyProblem, logits, tokens, uniform=None, draft=None, stream=None) -> None:
+    """tokens int32 [B][S]: the rows' drafted tokens (row 0's is not read); uniform float32
+    [B][S] in [0, 1): row r's test, and row 0's draw (None where temperature is 0)."""
+    _expect_device(prob, stream)
+    _expect_layout(prob, "logits", logits)
+    if (draft is None) != (prob.layout["draft"] is None):
+        raise ValueError("draft must be given where the problem was prepared with it, and only there")
+    if draft is not None:
+        _expect_layout(prob, "draft", draft)
+    dev = prob.ws.device
+    _expect("tokens", tokens, prob.layout["tokens"], torch.int32, dev)
+    if uniform is not None or prob.params.temperature != 0:
+        _expect("uniform", uniform, prob.layout["uniform"], torch.float32, dev)
+    verify(prob.ver, logits, tokens, uniform, draft, prob.path, prob.count, prob.next, prob.row_weight,
+           prob.ws, stream)
 
 
 # ---------------------------------------------------------------------------
