@@ -634,11 +634,23 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     }
     return;
   }
+  // The blocks of a (layer, KV head) are its sequences' side by side, as they lie in the
+  // cache: sequence b's begin behind seq_off[b] / kJoinTokens + b others, which is room for
+  // the last, partial one of each. (A block for each of the longest in every sequence: 8 units
+  // of 131072 tokens beside 56 of 31 to 32768, 21 us, 14.6 so.) Offsets that go back and
+  // forth may put blocks of several sequences here.
   const int item = blockIdx.x - rows_grid;
-  const int u = item / token_blocks, blk = item - u * token_blocks;
-  const Unit un = attention_unit(g, at, u);
-  const int t0 = blk * kJoinTokens;
-  if (t0 >= un.n && blk > 0) return;
+  const int lh = item / token_blocks, place = item - lh * token_blocks;
+  for (int b0 = 0; b0 < g.B; b0 += 64) {
+  const int lane = tid & 63;
+  const int2 held = b0 + lane < g.B ? sequence_rows(g, at, b0 + lane) : int2{0, -1};
+  const int first = (int)(min(max((int64_t)held.x, (int64_t)0), g.T) / kJoinTokens) + b0 + lane;
+  const int blocks = held.y < 0 ? 0 : max(1, (held.y + kJoinTokens - 1) / kJoinTokens);
+  uint64_t here = __ballot(place >= first && place < first + blocks);
+  for (; here; here &= here - 1) {
+  const int i = __builtin_ctzll(here), b = b0 + i, u = b * g.L * g.H + lh;
+  const Unit un = {b, lh / g.H, lh % g.H, 0, __builtin_amdgcn_readlane(held.x, i), __builtin_amdgcn_readlane(held.y, i)};
+  const int blk = place - __builtin_amdgcn_readlane(first, i), t0 = blk * kJoinTokens;
   // The entries and the rows' logits are requested before the rows' lse is joined.
   // Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
   const int64_t tr = token_row(g, un) + t0;
@@ -713,6 +725,9 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
         sum = __builtin_fmaf(sw[r], exp2_fast(p.zd[((int64_t)u * R + r) * S + tid] - slse[r]), sum);
     p.acc_draft[(int64_t)u * S + tid] = sum;
   }
+  __syncthreads();  // the rows' lse is read before another block's is written
+  }
+  }
 }
 
 template <typename T, int D>
@@ -731,8 +746,8 @@ static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, int grou
   const int few = wide ? w.splits <= kJoinFew : UR > kJoinRows;
   const int64_t per = few ? kThreads / (D / 4) : 1;
   const int rows_grid = wide && w.splits == 1 ? 0 : (int)((UR + per - 1) / per);
-  const int token_blocks = std::max(1, (g.maxn + kJoinTokens - 1) / kJoinTokens);
-  const int64_t grid = rows_grid + (w.keep ? (int64_t)g.U * token_blocks : 0);
+  const int token_blocks = (int)(g.T / kJoinTokens) + g.B;  // of a (layer, KV head)
+  const int64_t grid = rows_grid + (w.keep ? (int64_t)g.L * g.H * token_blocks : 0);
   auto go = [&](auto kern) {
     kern<<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, jg, few, rows_grid, token_blocks);
   };

@@ -97,7 +97,7 @@ struct QuantParams {
 
 // 16-token tiles of a step.
 template <typename T, int D, int MT>
-constexpr int kStepTiles = MT == 2 ? 2 : 4;
+constexpr int kStepTiles = 2;
 
 }  // namespace
 
@@ -236,6 +236,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
   const auto acc_range = buffer_range(accb + t0, 4 * max(0, t1 - t0));
   auto load_acc = [&](int r0) { return buffer_load_f32(acc_range, 4 * (r0 - t0 + (lane & (STEP - 1)))); };
   const auto keep_range = buffer_range(p.z + keep_at(g, un, R, t0 / 16), (t1 - t0 + 15) / 16 * R * 64);
+  // (rows past R: past the range's end at any step, by an addition where a choice of the
+  // offset would be a branch around each store)
+  const int keep_at_lane = row[0] < R ? row[0] * 64 + qg * 16 : INT32_MAX / 2;
 
   // The softmax's step over N tiles of logits: raises the maxima where it has to, leaves
   // the weights in z and adds them to the sums.
@@ -323,16 +326,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
           for (int i = 0; i < MT; ++i) z[i][t][e] = see ? z[i][t][e] : -INFINITY;
         }
     }
+    f32x4 keep[MODE == kKeeps ? NT : 1];
     if constexpr (MODE == kKeeps) {
       // in powers of two, for the accumulation
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        f32x4 x;
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = z[0][t][e] * at.c;
-        buffer_store16(keep_range, row[0] < R ? (((r0 - t0) / 16 + t) * R + row[0]) * 64 + qg * 16 : INT32_MAX - 15,
-                       x);
-      }
+        for (int e = 0; e < 4; ++e) keep[t][e] = z[0][t][e] * at.c;
     }
     soft(std::integral_constant<int, NT>{}, z);
 #pragma unroll
@@ -365,6 +365,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
         }
     }
     fetch_v();
+    if constexpr (MODE == kKeeps) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        buffer_store16(keep_range, keep_at_lane + ((r0 - t0) / 16 + t) * R * 64, keep[t]);
+    }
   };
 
   // A step over drafted tokens d0 .., each row seeing those of its mask only: their rows are in
@@ -495,11 +500,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
   // drafted tokens' steps.
   const int dsteps = drafts ? (S + W::kStep - 1) / W::kStep : 0;
   int r0 = t0 + ((wave - dsteps) & 3) * STEP;  // the wave's first step of the chunk
+  // (requested in the order of the loop's steps: the waits before the loop and in it are for
+  // the same number of later loads)
   load_k(r0);
-  load_v(r0);
   float2 sc = load_scales(r0);
   float a = 0.0f;
   if constexpr (HIDES) a = load_acc(r0);
+  load_v(r0);
   for (int s = wave; s < dsteps; s += 4) draft_step(s * W::kStep);
   for (; r0 < t1; r0 += 4 * STEP) {
     const int next = r0 + 4 * STEP, rows = min(STEP, t1 - r0);
@@ -591,13 +598,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
 }
 
 // ---------------------------------------------------------------------------
-// The weights that rows of known lse gave the cached tokens. A wave holds the keys of 64
-// tokens as operands and passes the rows that count by them, 16 at a time, from LDS: those
-// of weight 0 (a verified tree's rejected rows, mostly) are left out before any product. A
-// lane's sums are of its own row and 4 tokens a tile, the 16 rows' joined at the end; each
-// token's sum is one wave's, in the rows' order.
+// The weights that rows of known lse gave the cached tokens. A workgroup lists the rows that
+// count (those of weight 0, mostly a verified tree's rejected ones, are left out before any
+// product) and holds the first of them as operands in LDS; then a stretch of a unit's
+// tokens passes them, 64 a wave at a time, the next ones' codes requested meanwhile. A lane's
+// sums are of its own row and 4 tokens a tile, the 16 rows' joined at the end; each token's
+// sum is one wave's, in the rows' order.
 // ---------------------------------------------------------------------------
-constexpr int kSumList = 1024;  // rows listed at a time
+constexpr int kSumList = 1024;          // rows listed at a time
+constexpr int kSumLds = 40 * 1024;      // of operands: three workgroups to a compute unit
+constexpr int kSumTokens = 256;         // of a workgroup at a time
+constexpr int kQuantSumBlocks = 768;    // workgroups that the stretches are cut for
 
 template <typename T>
 struct QuantSumArgs {
@@ -608,111 +619,149 @@ struct QuantSumArgs {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void quant_sum_kernel(Geo g, Attn at, QuantArgs qa, QuantSumArgs<T> p,
-                                                                int blocks) {
-  constexpr int TERMS = kTerms<T>, NT = 4, TOKENS = 16 * NT;
+__global__ __launch_bounds__(kThreads, 3) void quant_sum_kernel(Geo g, Attn at, QuantArgs qa, QuantSumArgs<T> p,
+                                                                int blocks, int stretch) {
+  constexpr int TERMS = kTerms<T>, NT = 4, TOKENS = 16 * NT, OPS = D / 32;
+  constexpr int HELD = kSumLds / (TERMS * OPS * 1024);  // 16-row tiles in LDS
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (blockIdx.x == 0 && p.status) write_status(g, at, p.status);
   const int u = blockIdx.x / blocks, blk = blockIdx.x - u * blocks;
   const Unit un = attention_unit(g, at, u);
-  const int b0 = blk * 4 * TOKENS, r0 = b0 + wave * TOKENS;
-  if (b0 >= un.n) return;
+  const int s0 = blk * stretch, s1 = min(un.n, s0 + stretch);
+  if (s0 >= s1) return;
   const int S = g.w, R = at.R;
-  __shared__ int list[kSumList];        // rows of weight not 0, lse not -inf
-  __shared__ float2 row[kSumList];      // their lse (in powers of two), weight
+  __shared__ __align__(16) uint4 ops[HELD * TERMS * OPS * 64];
+  __shared__ int list[kSumList];                  // rows of weight not 0, lse not -inf
+  __shared__ float2 row[kSumList];                // their lse (in powers of two), weight
   __shared__ int counts[4];
-  const int left = un.n - r0;
-  // keys, scales and accumulators
+  const uint8_t* kb = qa.k + un.l * g.ksl + un.h * g.ksh + un.t0 * g.kst;
+  const auto sr = scale_range(qa, g, un, un.n);
+  const int64_t tr = token_row(g, un);
   uint4 kf[NT][D / 64];
-  {
+  float old, scale;  // of lane's token; of tile lane % NT
+  auto load = [&](int r0) {
     const int32_t bytes = (int32_t)g.kst;
-    const uint8_t* kb = qa.k + un.l * g.ksl + un.h * g.ksh + (un.t0 + r0) * g.kst;
-    const auto rs = buffer_range(kb, rows_bytes(min(TOKENS, left), bytes, D));
+    const auto rs = buffer_range(kb + r0 * g.kst, rows_bytes(min(TOKENS, s1 - r0), bytes, D));
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int a = 0; a < D / 64; ++a) kf[t][a] = buffer_load16(rs, (16 * t + m) * bytes + 64 * a + 16 * qg);
-  }
-  const auto sr = scale_range(qa, g, un, un.n);
-  float scale[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) scale[t] = buffer_load_f32(sr, (r0 + 16 * t) >> qa.shift << 3);
-  const auto ar = buffer_range(p.acc + token_row(g, un) + r0, 4 * max(0, min(TOKENS, left)));
-  const float old = buffer_load_f32(ar, 4 * lane);
-  float sum[NT][4];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[t][e] = 0.0f;
+    scale = buffer_load_f32(sr, (r0 + 16 * (lane & (NT - 1))) >> qa.shift << 3);
+    old = buffer_load_f32(buffer_range(p.acc + tr + r0, 4 * max(0, min(TOKENS, s1 - r0))), 4 * lane);
+  };
+  int r0 = s0 + wave * TOKENS;
+  load(r0);
 
   const T* qu = unit_queries(g, un, p.q);
   const float* lse = p.lse + (int64_t)u * R;
-  for (int first = 0; first < R; first += kSumList) {
-    // the rows that count, in order
-    int n = 0;
+  int n = 0;  // rows listed
+  auto make_list = [&](int first) {
+    n = 0;
     __syncthreads();
-    for (int x = first; x < min(R, first + kSumList); x += kThreads) {
+    const int end = min(R, first + kSumList);
+    for (int x = first; x < end; x += kThreads) {
       const int r = x + tid;
       float w = 0.0f, ls = 0.0f;
-      if (r < min(R, first + kSumList)) {
+      if (r < end) {
         ls = lse[r];
         w = at.row_weight ? at.row_weight[(int64_t)un.b * S + r % S] : 1.0f;
       }
-      const bool counts_ = w != 0.0f && ls != -INFINITY;
-      const uint64_t mask = __ballot(counts_);
+      const bool takes = w != 0.0f && ls != -INFINITY;
+      const uint64_t mask = __ballot(takes);
       if (lane == 0) counts[wave] = __builtin_popcountll(mask);
       __syncthreads();
-      int at_ = n;
+      int to = n;
       for (int y = 0; y < 4; ++y) {
-        if (y < wave) at_ += counts[y];
+        if (y < wave) to += counts[y];
         n += counts[y];
       }
-      if (counts_) {
-        at_ += __builtin_popcountll(mask & ((1ull << lane) - 1));
-        list[at_] = r;
-        row[at_] = float2{ls * kLog2e, w};
+      if (takes) {
+        to += __builtin_popcountll(mask & ((1ull << lane) - 1));
+        list[to] = r;
+        row[to] = float2{ls * kLog2e, w};
       }
       __syncthreads();
     }
-    if (left <= 0) continue;
-    for (int x = 0; x < n; x += 16) {
-      const bool used = x + m < n;
-      const int i = min(x + m, n - 1);
-      const float2 rw = row[i];
-      uint4 qf[TERMS][D / 32];
-      load_query<T, D>(g, qu, list[i], used, qg, qf);
+    // the last tile's padding: queries of 0 and the weight 0
+    if (tid < 16 && n + tid < kSumList) row[n + tid] = float2{0.0f, 0.0f};
+    for (int x = wave; x < HELD && 16 * x < n; x += 4) {
+      uint4 f[TERMS][OPS];
+      load_query<T, D>(g, qu, list[min(16 * x + m, n - 1)], 16 * x + m < n, qg, f);
+#pragma unroll
+      for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+        for (int a = 0; a < OPS; ++a) ops[((x * TERMS + i) * OPS + a) * 64 + lane] = f[i][a];
+    }
+    __syncthreads();
+  };
+  for (int b0 = s0; b0 < s1; b0 += kSumTokens, r0 += kSumTokens) {
+    float sum[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[t][e] = 0.0f;
+    for (int first = 0; first < R; first += kSumList) {
+      if (b0 == s0 || R > kSumList) make_list(first);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const f32x4 z = quant_logits<TERMS, D>(kf[t], scale[t], qf);
+        if (r0 + 16 * t >= s1) continue;
+        uint4 op[OPS];
+        const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), t));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float w = exp2_fast(__builtin_fmaf(z[e], at.c, -rw.x));
-          sum[t][e] = used ? __builtin_fmaf(rw.y, w, sum[t][e]) : sum[t][e];
+        for (int a = 0; a < D / 64; ++a) {
+          op[2 * a] = widen8(kf[t][a].x, kf[t][a].y, sc);
+          op[2 * a + 1] = widen8(kf[t][a].z, kf[t][a].w, sc);
+        }
+        for (int x = 0; 16 * x < n; ++x) {
+          uint4 q[TERMS][OPS];
+          if (x < HELD) {
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+              for (int a = 0; a < OPS; ++a) q[i][a] = ops[((x * TERMS + i) * OPS + a) * 64 + lane];
+          } else {
+            load_query<T, D>(g, qu, list[min(16 * x + m, n - 1)], 16 * x + m < n, qg, q);
+          }
+          const float2 rw = row[16 * x + m];
+          f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = TERMS - 1; i >= 0; --i)
+#pragma unroll
+            for (int a = 0; a < OPS; ++a)
+              z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, op[a]),
+                                                          __builtin_bit_cast(bf8, q[i][a]), z, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sum[t][e] = __builtin_fmaf(rw.y, exp2_fast(__builtin_fmaf(z[e], at.c, -rw.x)), sum[t][e]);
         }
       }
     }
+    const float was = old;
+    const int left = s1 - r0;
+    if (b0 + kSumTokens < s1) load(r0 + kSumTokens);
+    // the rows' sums of each token, in every lane of its group of 16
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum[t][e] += dpp_f32<kDppQuadXor1>(sum[t][e]);
+        sum[t][e] += dpp_f32<kDppQuadXor2>(sum[t][e]);
+        sum[t][e] += dpp_f32<kDppHalfMirror>(sum[t][e]);
+        sum[t][e] += dpp_f32<kDppMirror>(sum[t][e]);
+      }
+    // lane j takes token j: tile j / 16, lane group j / 4 % 4, entry j % 4
+    float mine = 0.0f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int e = lane & 3;
+      const float x = e == 0 ? sum[t][0] : e == 1 ? sum[t][1] : e == 2 ? sum[t][2] : sum[t][3];
+      const float y = __shfl(x, 16 * (lane >> 2 & 3) + e);
+      mine = t == lane >> 4 ? y : mine;
+    }
+    if (lane < left && !(was < 0.0f))
+      p.acc[tr + r0 + lane] = at.decay > 0.0f ? __builtin_fmaf(at.decay, was, mine) : mine;
   }
-  if (left <= 0) return;
-  // the rows' sums of each token: lane 16 q + m of a tile's tokens 4 q ..
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) sum[t][e] += __shfl_xor(sum[t][e], o);
-    }
-  // lane j takes token j: tile j / 16, lane group j / 4 % 4, entry j % 4
-  float mine = 0.0f;
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = __shfl(sum[t][e], 16 * (lane >> 2 & 3));
-      mine = t == lane >> 4 && e == (lane & 3) ? x : mine;
-    }
-  if (lane < left && !(old < 0.0f))
-    p.acc[token_row(g, un) + r0 + lane] = at.decay > 0.0f ? __builtin_fmaf(at.decay, old, mine) : mine;
 }
 
 template <typename T, int D>
@@ -773,13 +822,23 @@ int attend_quant_group(const AttnLaunch& A, const AttendSpace& w) {
   return 64 * (w.mt == 2 ? kStepTiles<__bf16, 128, 2> : kStepTiles<__bf16, 128, 1>);
 }
 
+// Tokens of a workgroup of the sums: an equal part for each of kQuantSumBlocks, in whole rounds of
+// its waves; one round where the rows are listed again for each.
+static int quant_sum_stretch(const AttnLaunch& A) {
+  const Geo& g = A.base.geo;
+  if (A.at.R > kSumList) return kSumTokens;
+  const int64_t per = (int64_t)g.L * g.H * g.T / kQuantSumBlocks / kSumTokens * kSumTokens;
+  return (int)std::min<int64_t>(std::max<int64_t>(per, kSumTokens), 1 << 20);
+}
+
 template <typename T, int D>
 static hipError_t quant_sum_typed(const QuantLaunch& A, const void* q, const float* lse, float* acc,
                                   uint32_t* status) {
   const Geo& g = A.attn.base.geo;
-  const int blocks = std::max(1, (g.maxn + kThreads - 1) / kThreads);  // of 256 tokens
+  const int stretch = quant_sum_stretch(A.attn);
+  const int blocks = std::max(1, (g.maxn + stretch - 1) / stretch);
   quant_sum_kernel<T, D><<<(unsigned)((int64_t)g.U * blocks), kThreads, 0, A.attn.base.stream>>>(
-      g, A.attn.at, A.q, QuantSumArgs<T>{(const T*)q, lse, acc, status}, blocks);
+      g, A.attn.at, A.q, QuantSumArgs<T>{(const T*)q, lse, acc, status}, blocks, stretch);
   return hipGetLastError();
 }
 

@@ -14,6 +14,7 @@ namespace jacap {
 namespace {
 
 constexpr int kQuantTokens = 128;  // per workgroup: the largest block
+constexpr int kFewAppend = 4;      // tokens of a call up to which one wave takes a unit
 constexpr uint32_t kInfBits = 0x7F800000u;
 
 // The exponent for a block whose largest finite magnitude has these bits (fp32).
@@ -198,32 +199,43 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(Geo g, Attn at, Quan
 // need, the blocks' new exponents (of the block's first token here: the largest of those
 // that go to it and its own), the codes of blocks whose scale has grown rounded again, and
 // the tokens' codes.
+// Up to kFewAppend tokens by one wave, so that more units are in flight (4096 units of one
+// token: 14.8 us by four waves, 7.0 so); the chain of loads (the tokens' places, their rows and scales) is what
+// such a call takes.
 template <typename T, int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void append_kernel(Geo g, Attn at, QuantArgs qa, AppendArgs p,
                                                          const T* kd, const T* vd, uint8_t* kq,
                                                          uint8_t* vq, float2* scales) {
   using S = Spread<T, D>;
   constexpr int GROUPS = THREADS / S::kLanes;  // groups of lanes that take a row each
+  constexpr int MOST = THREADS == 64 ? kFewAppend : kMaxAppend;
+  constexpr int PER = (MOST + THREADS - 1) / THREADS;
   const int tid = threadIdx.x, S_ = g.w;
   const Unit un = decode_unit(g, blockIdx.x);
   const int rows = whole_blocks(g, at, un.b) ? un.n : 0;
-  __shared__ int pos[kMaxAppend];                // -1: not written
-  __shared__ int16_t src[kMaxAppend];
-  __shared__ int16_t need[2][kMaxAppend];        // exponents: the row's, then its block's new one
-  __shared__ int16_t fell[2][kMaxAppend];        // how far the block's codes fall (its first token)
+  __shared__ int pos[MOST];                      // -1: not written
+  __shared__ int16_t src[MOST];
+  __shared__ int16_t need[2][MOST];              // exponents: the row's, then its block's new one
+  __shared__ int16_t fell[2][MOST];              // how far the block's codes fall (its first token)
   const int m = p.count ? min(max(p.count[un.b], 0), S_) : S_;
   const int64_t start = p.start ? p.start[un.b] : 0;
   if (p.start_out && p.start_out != p.start && un.l == 0 && un.h == 0 && tid == 0)
     p.start_out[un.b] = (int32_t)start + m;
   if (m == 0) return;
   bool bad = false;
-  for (int j = tid; j < m; j += THREADS) {
+  float2* const sc = scales + ((int64_t)un.l * g.H + un.h) * (g.T >> qa.shift) + (un.t0 >> qa.shift);
+  float2 held[PER];  // the scales of the tokens' blocks
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int j = tid + x * THREADS;
+    if (j >= m) continue;
     const int64_t place = start + j;
     int64_t to = place;
     if (p.slots) to = place >= 0 && place < p.slot_cap ? p.slots[(int64_t)blockIdx.x * p.slot_cap + place] : -1;
     const int r = p.rows ? p.rows[un.b * (int64_t)S_ + j] : j;
     const bool ok = to >= 0 && to < rows && (uint32_t)r < (uint32_t)S_;
     bad |= !ok;
+    if (ok) held[x] = sc[to >> qa.shift];
     pos[j] = ok ? (int)to : -1;
     src[j] = (int16_t)(ok ? r : 0);
   }
@@ -251,7 +263,6 @@ __global__ __launch_bounds__(THREADS) void append_kernel(Geo g, Attn at, QuantAr
   __syncthreads();
   // Of two tokens for one position the later is written.
   if (p.slots && m > 1) {
-    constexpr int PER = (kMaxAppend + THREADS - 1) / THREADS;
     uint32_t again = 0;
     for (int x = 0, j = tid; x < PER && j < m; ++x, j += THREADS)
       for (int y = j + 1; y < m; ++y)
@@ -261,10 +272,8 @@ __global__ __launch_bounds__(THREADS) void append_kernel(Geo g, Attn at, QuantAr
       if (again >> x & 1) pos[j] = -1;
     __syncthreads();
   }
-  float2* const sc = scales + ((int64_t)un.l * g.H + un.h) * (g.T >> qa.shift) + (un.t0 >> qa.shift);
   {
     // (read by all before any is written: the rows' own exponents are in `need` until then)
-    constexpr int PER = (kMaxAppend + THREADS - 1) / THREADS;
     int16_t e[2][PER], old[2][PER];
     bool lead[PER];
 #pragma unroll
@@ -272,7 +281,7 @@ __global__ __launch_bounds__(THREADS) void append_kernel(Geo g, Attn at, QuantAr
       const int j = tid + x * THREADS;
       if (j >= m || pos[j] < 0) continue;
       const int block = pos[j] >> qa.shift;
-      const float2 s = sc[block];
+      const float2 s = held[x];
       lead[x] = true;
       for (int i = 0; i < 2; ++i)
         e[i][x] = old[i][x] = (int16_t)((int)(__float_as_uint(i ? s.y : s.x) >> 23 & 0xFF) - 127);
@@ -378,7 +387,8 @@ static hipError_t append_typed(const QuantLaunch& A, const AppendArgs& p, const 
     kern<<<(unsigned)g.U, threads, 0, A.attn.base.stream>>>(g, A.attn.at, A.q, p, (const T*)kd, (const T*)vd,
                                                             (uint8_t*)kq, (uint8_t*)vq, (float2*)scales);
   };
-  go(append_kernel<T, D, kThreads>, kThreads);
+  if (g.w <= kFewAppend) go(append_kernel<T, D, 64>, 64);
+  else go(append_kernel<T, D, kThreads>, kThreads);
   return hipGetLastError();
 }
 

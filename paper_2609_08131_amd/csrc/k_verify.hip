@@ -21,29 +21,89 @@ namespace {
 constexpr int kSliceVecs = kVerifyThreads * kVerifyVecs;
 
 // A row of V logits as 16-byte pieces: piece v holds elements v VE - off .., off that of the
-// row's first in its own.
+// row's first in its own. lo .. hi are the pieces inside the row.
 template <typename T>
 struct LogitRow {
   static constexpr int VE = 16 / (int)sizeof(T);
   const T* base;
-  int off, V, pieces;
+  int off, V, pieces, lo, hi;
   __device__ __forceinline__ LogitRow(const T* row, int V_) : base(row), V(V_) {
     off = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
     pieces = (off + V + VE - 1) / VE;
+    lo = off > 0 ? 1 : 0;
+    hi = (off + V) / VE - 1;
   }
-  // The piece's logits as fp32; -inf outside the row.
-  __device__ __forceinline__ void load(int v, float (&x)[VE]) const {
-    const int x0 = v * VE - off;
-    if (x0 >= 0 && x0 + VE <= V) {
-      const uint4 y = *reinterpret_cast<const uint4*>(base + x0);
-      const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+  __device__ __forceinline__ bool inside(int v) const { return v >= lo && v <= hi; }
+  // Pieces v0, v0 + step ... as fp32, -inf outside the row. The loads are requested together,
+  // with no branch between them (a branch each, and each was waited for: 1024 rows of
+  // 128256 62 us, 46 so: 5.8 TB/s); a piece at an end of the row is put in afterwards.
+  template <int N>
+  __device__ __forceinline__ void load(int v0, int step, float (&x)[N][VE]) const {
+    uint4 y[N];
+    if (lo <= hi) {
 #pragma unroll
-      for (int i = 0; i < VE; ++i)
-        x[i] = sizeof(T) == 4 ? __uint_as_float(w[i * (int)sizeof(T) / 4])
-                              : __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+      for (int i = 0; i < N; ++i)
+        y[i] = *reinterpret_cast<const uint4*>(base + min(max(v0 + i * step, lo), hi) * VE - off);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint32_t w[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+        const bool in = inside(v0 + i * step);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const uint32_t u = sizeof(T) == 4 ? w[e * (int)sizeof(T) / 4]
+                                            : (e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16;
+          x[i][e] = in ? __uint_as_float(u) : -INFINITY;
+        }
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < VE; ++i) x[i] = x0 + i >= 0 && x0 + i < V ? (float)base[x0 + i] : -INFINITY;
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) x[i][e] = -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int v = v0 + i * step;
+      if (v >= 0 && v < pieces && !inside(v)) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const int at = v * VE - off + e;
+          if (at >= 0 && at < V) x[i][e] = (float)base[at];
+        }
+      }
+    }
+  }
+  // The same of the draft's probabilities q of the row (0 outside).
+  template <int N>
+  __device__ __forceinline__ void load_draft(const float* q, int v0, int step, float (&x)[N][VE]) const {
+    const bool whole = (reinterpret_cast<uintptr_t>(q - off) & 15) == 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int v = v0 + i * step, first = min(max(v, lo), hi) * VE - off;
+      if (whole && lo <= hi) {
+#pragma unroll
+        for (int e = 0; e < VE; e += 4) {
+          const float4 y = *reinterpret_cast<const float4*>(q + first + e);
+          x[i][e] = y.x;
+          x[i][e + 1] = y.y;
+          x[i][e + 2] = y.z;
+          x[i][e + 3] = y.w;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) x[i][e] = q[min(max(v * VE - off + e, 0), V - 1)];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int v = v0 + i * step;
+      if (!inside(v)) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const int at = v * VE - off + e;
+          x[i][e] = at >= 0 && at < V ? q[at] : 0.0f;
+        }
+      }
     }
   }
 };
@@ -69,74 +129,104 @@ __device__ __forceinline__ T block_all(T v, T* red, Op op) {
   return r;
 }
 
-struct Best {
-  float top;
-  int at;
-};
-__device__ __forceinline__ Best better(const Best& a, const Best& b) {
-  return b.top > a.top || (b.top == a.top && b.at < a.at) ? b : a;
+// A piece's values added pair by pair.
+template <int N>
+__device__ __forceinline__ float add_pairs(const float (&x)[N]) {
+  float y[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) y[i] = x[2 * i] + x[2 * i + 1];
+  if constexpr (N == 2) return y[0];
+  else return add_pairs(y);
+}
+
+// The largest of two parts, and their sums in units of it. (A part of -inf only has the sum
+// 0; one with a NaN or +inf a NaN, which stays.)
+__device__ __forceinline__ void join(float& top, double& sum, float t, double s, float k) {
+  const float now = fmaxf(top, t);
+  sum = (sum == 0.0 ? 0.0 : sum * (double)expo(top, now, k)) + (s == 0.0 ? 0.0 : s * (double)expo(t, now, k));
+  top = now;
 }
 
 }  // namespace
 
+// A wave keeps kRowVecs pieces a lane in registers between its own maximum and its sum: the
+// waves meet once, at the end. Eight exponentials are added in fp32 pair by pair (three
+// roundings beside their own), the rest in fp64: a conversion and an addition for each would be
+// as much vector work as the exponentials.
 template <typename T, bool GREEDY>
 __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch p) {
   using Row = LogitRow<T>;
-  constexpr int VE = Row::VE;
-  const int tid = threadIdx.x;
-  const int row = blockIdx.x / p.slices, slice = blockIdx.x - row * p.slices;
+  constexpr int VE = Row::VE, WAVES = kVerifyThreads / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row = blockIdx.x / p.row_slices, slice = blockIdx.x - row * p.row_slices;
   const int b = row / p.S, r = row - b * p.S;
   if (blockIdx.x == 0) {
     for (int i = tid; i < p.B; i += kVerifyThreads) p.arrived[i] = 0;
     if (tid == 0) *p.status = 0;
   }
   const Row z((const T*)p.logits + b * p.lss + r * p.lsr, p.V);
-  float x[kVerifyVecs][VE];
-#pragma unroll
-  for (int i = 0; i < kVerifyVecs; ++i) {
-    const int v = slice * kSliceVecs + i * kVerifyThreads + tid;
-    if (v < z.pieces) {
-      z.load(v, x[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < VE; ++e) x[i][e] = -INFINITY;
-    }
-  }
+  const int v0 = (slice * WAVES + wave) * kRowVecs * 64 + lane;
+  float x[kRowVecs][VE];
+  z.load(v0, 64, x);
   RowPart* part = p.parts + blockIdx.x;
   if constexpr (GREEDY) {
-    Best best{-INFINITY, INT32_MAX};
+    float top = -INFINITY;
+    int at = INT32_MAX;
 #pragma unroll
-    for (int i = 0; i < kVerifyVecs; ++i)
+    for (int i = 0; i < kRowVecs; ++i)
 #pragma unroll
       for (int e = 0; e < VE; ++e)
-        if (x[i][e] > best.top)  // (never a NaN; pieces in ascending order)
-          best = Best{x[i][e], (slice * kSliceVecs + i * kVerifyThreads + tid) * VE - z.off + e};
+        if (x[i][e] > top) {  // (never a NaN; in ascending order)
+          top = x[i][e];
+          at = (v0 + 64 * i) * VE - z.off + e;
+        }
+    auto take = [&](float t, int a) {
+      const bool more = t > top || (t == top && a < at);
+      top = more ? t : top;
+      at = more ? a : at;
+    };
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) best = better(best, Best{__shfl_xor(best.top, o), __shfl_xor(best.at, o)});
-    __shared__ Best red[kVerifyThreads / 64];
-    if ((tid & 63) == 0) red[tid >> 6] = best;
+    for (int o = 32; o > 0; o >>= 1) take(__shfl_xor(top, o), __shfl_xor(at, o));
+    __shared__ float tops[WAVES];
+    __shared__ int ats[WAVES];
+    if (lane == 0) {
+      tops[wave] = top;
+      ats[wave] = at;
+    }
     __syncthreads();
     if (tid == 0) {
-      for (int i = 1; i < kVerifyThreads / 64; ++i) best = better(best, red[i]);
-      *part = RowPart{best.top, best.at, 0.0};
+      for (int i = 1; i < WAVES; ++i) take(tops[i], ats[i]);
+      *part = RowPart{top, at, 0.0};
     }
   } else {
-    __shared__ float redf[kVerifyThreads / 64];
-    __shared__ double redd[kVerifyThreads / 64];
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kVerifyVecs; ++i)
+    for (int i = 0; i < kRowVecs; ++i)
 #pragma unroll
       for (int e = 0; e < VE; ++e) top = fmaxf(top, x[i][e]);
-    top = block_all(top, redf, [](float a, float c) { return fmaxf(a, c); });
-    const float ref = top == -INFINITY ? 0.0f : top;  // (a slice of -inf: its sum is 0)
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float ref = top == -INFINITY ? 0.0f : top;  // (a wave's all -inf: its sum is 0)
     double sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < kVerifyVecs; ++i)
+    for (int i = 0; i < kRowVecs; ++i) {
 #pragma unroll
-      for (int e = 0; e < VE; ++e) sum += (double)expo(x[i][e], ref, p.k);
-    sum = block_all(sum, redd, [](double a, double c) { return a + c; });
-    if (tid == 0) *part = RowPart{top, 0, sum};
+      for (int e = 0; e < VE; ++e) x[i][e] = expo(x[i][e], ref, p.k);
+      sum += (double)add_pairs(x[i]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    __shared__ float tops[WAVES];
+    __shared__ double sums[WAVES];
+    if (lane == 0) {
+      tops[wave] = top;
+      sums[wave] = sum;
+    }
+    __syncthreads();
+    if (tid == 0) {
+      for (int i = 1; i < WAVES; ++i) join(top, sum, tops[i], sums[i], p.k);
+      *part = RowPart{top, 0, sum};
+    }
   }
 }
 
@@ -149,7 +239,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
   const int slices = GREEDY ? 1 : p.slices;
   const int b = blockIdx.x / slices, slice = blockIdx.x - b * slices;
   const int S = p.S;
-  __shared__ float top[kMaxVerifyRows];      // of a row
+  __shared__ float top[kMaxVerifyRows];      // a row's largest logit
   __shared__ double total[kMaxVerifyRows];   // ... its sum of exponentials (NaN: not to be used)
   __shared__ int16_t parent[kMaxVerifyRows]; // -1: not tested
   __shared__ int32_t token[kMaxVerifyRows];  // of a row; greedy: ...
@@ -166,27 +256,54 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
 
   const T* const logits = (const T*)p.logits + b * p.lss;
   const float* const draft = p.draft ? p.draft + b * p.qss : nullptr;
+  // A row's parent, token and number, and its token's logit at the parent (requested
+  // before the rows' statistics, which 16 lanes a row join).
   for (int r = tid; r < S; r += kVerifyThreads) {
-    const RowPart* parts = p.parts + ((int64_t)b * S + r) * p.slices;
-    float t = -INFINITY;
-    for (int i = 0; i < p.slices; ++i) t = fmaxf(t, parts[i].top);
-    if constexpr (GREEDY) {
-      int a = -1;
-      for (int i = p.slices - 1; i >= 0; --i)
-        if (parts[i].top == t && t > -INFINITY) a = parts[i].at;
-      best[r] = a;
-    } else {
-      double s = 0.0;
-      for (int i = 0; i < p.slices; ++i)
-        if (parts[i].sum != 0.0) s += parts[i].sum * (double)expo(parts[i].top, t, p.k);
-      total[r] = t > -INFINITY ? s : __builtin_nan("");
-    }
-    top[r] = t;
     const int up = r == 0 ? -1 : p.parents ? p.parents[(int64_t)b * S + r] : r - 1;
     const int x = r == 0 ? -1 : p.tokens[(int64_t)b * S + r];
-    parent[r] = (int16_t)(up >= 0 && up < r && (uint32_t)x < (uint32_t)p.V ? up : -1);
+    const bool tested = up >= 0 && up < r && (uint32_t)x < (uint32_t)p.V;
+    parent[r] = (int16_t)(tested ? up : -1);
     token[r] = x;
     taken[r] = r == 0;
+    if constexpr (!GREEDY) {
+      uniform[r] = p.uniform[(int64_t)b * S + r];
+      weight[r] = tested ? (float)logits[up * p.lsr + x] : 0.0f;
+      chance[r] = tested && draft ? draft[up * p.qsr + x] : 0.0f;
+    }
+  }
+  for (int r0 = 0; r0 < S; r0 += kVerifyThreads / 16) {
+    const int r = r0 + (tid >> 4);
+    const RowPart* parts = p.parts + ((int64_t)b * S + min(r, S - 1)) * p.row_slices;
+    float t = -INFINITY;
+    if constexpr (GREEDY) {
+      int a = INT32_MAX;
+      auto take = [&](float y, int z) {
+        if (y > t || (y == t && z < a)) {
+          t = y;
+          a = z;
+        }
+      };
+      for (int i = tid & 15; i < p.row_slices; i += 16) take(parts[i].top, parts[i].at);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) take(__shfl_xor(t, o), __shfl_xor(a, o));
+      if ((tid & 15) == 0 && r < S) best[r] = t > -INFINITY ? a : -1;
+    } else {
+      double s = 0.0;
+      for (int i = tid & 15; i < p.row_slices; i += 16) {
+        const RowPart part = parts[i];
+        join(t, s, part.top, part.sum, p.k);
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) {
+        const float y = __shfl_xor(t, o);
+        const double z = __shfl_xor(s, o);
+        join(t, s, y, z, p.k);
+      }
+      if ((tid & 15) == 0 && r < S) {
+        top[r] = t;
+        total[r] = t > -INFINITY ? s : __builtin_nan("");
+      }
+    }
   }
   if (tid == 0) {
     at_row = 0;
@@ -197,13 +314,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
   }
   __syncthreads();
   if constexpr (!GREEDY) {
-    for (int r = tid; r < S; r += kVerifyThreads) {
-      const int up = parent[r];
-      uniform[r] = p.uniform[(int64_t)b * S + r];
-      if (up < 0) continue;
-      weight[r] = expo((float)logits[up * p.lsr + token[r]], top[up], p.k);
-      chance[r] = draft ? draft[up * p.qsr + token[r]] : 0.0f;
-    }
+    for (int r = tid; r < S; r += kVerifyThreads)
+      if (parent[r] >= 0) weight[r] = expo(weight[r], top[parent[r]], p.k);
     if (tid == 0) left = total[0];
     __syncthreads();
   }
@@ -279,13 +391,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
       const Row z(logits + row * p.lsr, p.V);
       const float* q = draft + row * p.qsr;
       double sum = 0.0;
-      for (int v = tid; v < z.pieces; v += kVerifyThreads) {
-        float x[VE];
-        z.load(v, x);
-        const int x0 = v * VE - z.off;
+      for (int v = tid; v < z.pieces; v += kVerifyThreads * kVerifyVecs) {
+        float x[kVerifyVecs][VE], y[kVerifyVecs][VE];
+        z.load(v, kVerifyThreads, x);
+        z.load_draft(q, v, kVerifyThreads, y);
 #pragma unroll
-        for (int e = 0; e < VE; ++e)
-          if (x0 + e >= 0 && x0 + e < p.V) sum += rest((double)expo(x[e], top[row], p.k), c, (double)q[x0 + e]);
+        for (int i = 0; i < kVerifyVecs; ++i)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) sum += rest((double)expo(x[i][e], top[row], p.k), c, (double)y[i][e]);
       }
       sum = block_all(sum, redd, [](double a, double d) { return a + d; });
       if (tid == 0) left = sum;
@@ -316,34 +429,34 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     const float t = top[row];
     const double c = mult;
     const int n_gone = num_gone;
-    // Weights of a piece. The rejected tokens of a plain row are compared with its range.
-    auto weights = [&](int v, double mul, double (&w)[VE]) {
-      float x[VE];
-      z.load(v, x);
-      const int x0 = v * VE - z.off;
+    // The weights of pieces v0, v0 + step ... (0 outside the row), less the rejected tokens'.
+    auto weights = [&](int v0, int step, double mul, double (&w)[kVerifyVecs][VE]) __attribute__((always_inline)) {
+      float x[kVerifyVecs][VE], y[kVerifyVecs][VE];
+      z.load(v0, step, x);
+      if (mul != 0.0) z.load_draft(q, v0, step, y);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        w[e] = (double)expo(x[e], t, p.k);
-        if (mul != 0.0 && x0 + e >= 0 && x0 + e < p.V) w[e] = rest(w[e], mul, (double)q[x0 + e]);
-      }
-      for (int y = 0; y < n_gone; ++y) {
-        const int i = token[gone[y]] - x0;
+      for (int i = 0; i < kVerifyVecs; ++i)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) w[e] = i == e ? 0.0 : w[e];
+        for (int e = 0; e < VE; ++e) {
+          w[i][e] = (double)expo(x[i][e], t, p.k);
+          if (mul != 0.0) w[i][e] = rest(w[i][e], mul, (double)y[i][e]);
+        }
+      for (int g = 0; g < n_gone; ++g) {
+        const int x = token[gone[g]] + z.off, v = x / VE - v0;
+        if (v < 0 || v % step != 0 || v / step >= kVerifyVecs) continue;
+#pragma unroll
+        for (int i = 0; i < kVerifyVecs; ++i)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) w[i][e] = v / step == i && x % VE == e ? 0.0 : w[i][e];
       }
     };
-    auto slice_sum = [&](int s, double mul) {
-      double sum = 0.0;
+    auto slice_sum = [&](int s, double mul) __attribute__((always_inline)) {
+      double w[kVerifyVecs][VE], sum = 0.0;
+      weights(s * kSliceVecs + tid, kVerifyThreads, mul, w);
 #pragma unroll
-      for (int i = 0; i < kVerifyVecs; ++i) {
-        const int v = s * kSliceVecs + i * kVerifyThreads + tid;
-        if (v < z.pieces) {
-          double w[VE];
-          weights(v, mul, w);
+      for (int i = 0; i < kVerifyVecs; ++i)
 #pragma unroll
-          for (int e = 0; e < VE; ++e) sum += w[e];
-        }
-      }
+        for (int e = 0; e < VE; ++e) sum += w[i][e];
       return block_all(sum, redd, [](double a, double d) { return a + d; });
     };
     __shared__ int last;
@@ -359,8 +472,24 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     auto load_mass = [&](int s) {
       return __hip_atomic_load(&mass[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     };
+    // Their sum, and the slice in which the running one passes the goal (else the last of
+    // positive sum): 64 slices at a time in the lanes, each wave for itself.
     double mul = c, all = 0.0;
-    for (int s = 0; s < slices; ++s) all += load_mass(s);
+    auto scan = [&](double v) {
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(v, o);
+        if (lane >= o) v += y;
+      }
+      return v;
+    };
+    auto sum_all = [&] {
+      double run = 0.0;
+      for (int s = 0; s < slices; s += 64)
+        run += __shfl(scan(s + lane < slices ? load_mass(s + lane) : 0.0), 63);
+      return run;
+    };
+    all = sum_all();
     if (all == 0.0 && c > 0.0) {  // rounding left nothing: the row's own weights
       mul = 0.0;
       __syncthreads();
@@ -370,8 +499,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
       }
       __syncthreads();
       __threadfence();
-      all = 0.0;
-      for (int s = 0; s < slices; ++s) all += load_mass(s);
+      all = sum_all();
     }
     if (!(all > 0.0) || !(all < INFINITY)) {  // not a row to draw from
       if (tid == 0) {
@@ -380,54 +508,49 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
       }
       return;
     }
-    const double goal = (double)p.uniform[(int64_t)b * S] * all;
-    // The slice in which the running sum passes the goal (else the last of positive sum).
+    const double goal = (double)uniform[0] * all;
     int in = -1;
     double before = 0.0, run = 0.0;
-    for (int s = 0; s < slices; ++s) {
-      const double m = load_mass(s);
-      if (!(m > 0.0)) continue;
-      in = s;
-      before = run;
-      run += m;
-      if (run > goal) break;
+    for (int s = 0; s < slices; s += 64) {
+      const double m = s + lane < slices ? load_mass(s + lane) : 0.0;
+      const double incl = run + scan(m);
+      const uint64_t some = __ballot(m > 0.0), past = __ballot(m > 0.0 && incl > goal);
+      const uint64_t from = past ? past & -past : some;
+      if (from) {
+        const int i = 63 - __builtin_clzll(from);
+        in = s + i;
+        before = __shfl(incl - m, i);
+      }
+      if (past) break;
+      run = __shfl(incl, 63);
     }
     // Its pieces, kVerifyVecs in order to a thread.
-    double sum = 0.0;
+    double sum = 0.0, w[kVerifyVecs][VE];
     int final = -1;  // the last token of positive weight
     const int v0 = in * kSliceVecs + tid * kVerifyVecs;
-    for (int i = 0; i < kVerifyVecs && v0 + i < z.pieces; ++i) {
-      double w[VE];
-      weights(v0 + i, mul, w);
+    weights(v0, 1, mul, w);
+#pragma unroll
+    for (int i = 0; i < kVerifyVecs; ++i)
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        sum += w[e];
-        if (w[e] > 0.0) final = (v0 + i) * VE - z.off + e;
+        sum += w[i][e];
+        if (w[i][e] > 0.0) final = (v0 + i) * VE - z.off + e;
       }
-    }
-    double incl = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(incl, o);
-      if (lane >= o) incl += y;
-    }
+    const double incl_wave = scan(sum);
     __syncthreads();
-    if (lane == 63) redd[tid >> 6] = incl;
+    if (lane == 63) redd[tid >> 6] = incl_wave;
     __syncthreads();
     for (int i = 0; i < tid >> 6; ++i) before += redd[i];
+    const double incl = incl_wave;
     int found = INT32_MAX;
     double mass_to = before + (incl - sum);
-    if (before + incl > goal) {
-      for (int i = 0; i < kVerifyVecs && v0 + i < z.pieces && found == INT32_MAX; ++i) {
-        double w[VE];
-        weights(v0 + i, mul, w);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          mass_to += w[e];
-          if (w[e] > 0.0 && mass_to > goal && found == INT32_MAX) found = (v0 + i) * VE - z.off + e;
-        }
+    for (int i = 0; i < kVerifyVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        mass_to += w[i][e];
+        if (w[i][e] > 0.0 && mass_to > goal) found = min(found, (v0 + i) * VE - z.off + e);
       }
-    }
     found = block_all(found, redi, [](int a, int d) { return min(a, d); });
     __syncthreads();
     final = block_all(final, redi, [](int a, int d) { return max(a, d); });
@@ -437,7 +560,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
 
 template <typename T>
 static void rows_typed(const VerifyLaunch& A) {
-  const unsigned grid = (unsigned)((int64_t)A.B * A.S * A.slices);
+  const unsigned grid = (unsigned)((int64_t)A.B * A.S * A.row_slices);
   if (A.k > 0.0f) verify_rows_kernel<T, false><<<grid, kVerifyThreads, 0, A.stream>>>(A);
   else verify_rows_kernel<T, true><<<grid, kVerifyThreads, 0, A.stream>>>(A);
 }

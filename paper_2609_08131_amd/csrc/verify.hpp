@@ -7,7 +7,8 @@
 namespace jacap {
 
 constexpr int kVerifyThreads = 256;
-constexpr int kVerifyVecs = 4;      // 16-byte pieces of a row per thread
+constexpr int kRowVecs = 8;         // 16-byte pieces of a row per thread: of the rows' sums,
+constexpr int kVerifyVecs = 4;      // ... and of the draw
 constexpr int kMaxVerifyRows = 512;
 constexpr int kMaxVocab = 1 << 24;
 
@@ -33,15 +34,16 @@ struct VerifyLaunch {
   uint32_t* status;
   uint32_t* arrived;   // [B] slices of the draw that are summed
   double* mass;        // [B][slices]
-  RowPart* parts;      // [B][S][slices]
-  int slices;          // of a row
+  RowPart* parts;      // [B][S][row_slices]
+  int row_slices;      // of a row's sums,
+  int slices;          // ... and of the draw
   hipStream_t stream;
 };
 
 // Slices of a row of V logits: pieces of 16 bytes, one more where a row begins inside one.
-inline int verify_slices(int V, int dtype) {
+inline int verify_slices(int V, int dtype, int vecs) {
   const int per = dtype == JACAP_DTYPE_BF16 ? 8 : 4;
-  const int pieces = (V + 2 * (per - 1)) / per, slice = kVerifyThreads * kVerifyVecs;
+  const int pieces = (V + 2 * (per - 1)) / per, slice = kVerifyThreads * vecs;
   return (pieces + slice - 1) / slice;
 }
 

@@ -44,16 +44,18 @@ jacap_status check(const jacap_verification* v, VerifyLaunch* A, VerifySpace* w)
   A->qss = v->q_stride_seq;
   A->qsr = v->q_stride_row;
   A->parents = v->parents;
-  A->slices = verify_slices(v->vocab, v->dtype);
+  A->row_slices = verify_slices(v->vocab, v->dtype, kRowVecs);
+  A->slices = verify_slices(v->vocab, v->dtype, kVerifyVecs);
   const int64_t rows = (int64_t)A->B * A->S;
-  if (rows > kMaxVerifyGrid || rows * A->slices > kMaxVerifyGrid) return JACAP_ERR_UNSUPPORTED;
+  if (rows > kMaxVerifyGrid || rows * A->row_slices > kMaxVerifyGrid ||
+      (int64_t)A->B * A->slices > kMaxVerifyGrid) return JACAP_ERR_UNSUPPORTED;
   size_t o = 256;
   w->arrived = o;
   o = align256(o + 4 * (size_t)A->B);
   w->mass = o;
   o = align256(o + 8 * (size_t)A->B * A->slices);
   w->parts = o;
-  o = align256(o + sizeof(RowPart) * (size_t)rows * A->slices);
+  o = align256(o + sizeof(RowPart) * (size_t)rows * A->row_slices);
   w->total = o;
   return JACAP_OK;
 }
