@@ -19,6 +19,7 @@ namespace jacap {
 namespace {
 
 constexpr int kSliceVecs = kVerifyThreads * kVerifyVecs;
+constexpr int kRowLanes = 4;  // that join the parts of a row
 
 // A row of V logits as 16-byte pieces: piece v holds elements v VE - off .., off that of the
 // row's first in its own. lo .. hi are the pieces inside the row.
@@ -249,7 +250,6 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
   __shared__ uint8_t taken[kMaxVerifyRows];  // the row is accepted
   __shared__ int16_t gone[kMaxVerifyRows];   // rejected children of the current row
   __shared__ double redd[kVerifyThreads / 64];
-  __shared__ int redi[kVerifyThreads / 64];
   __shared__ float uniform[kMaxVerifyRows];  // its number
   __shared__ int at_row, at_next, num_gone, num_path;
   __shared__ double mult, left;              // C; N, what is left of the weights (greedy: not used)
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
   const T* const logits = (const T*)p.logits + b * p.lss;
   const float* const draft = p.draft ? p.draft + b * p.qss : nullptr;
   // A row's parent, token and number, and its token's logit at the parent (requested
-  // before the rows' statistics, which 16 lanes a row join).
+  // before the rows' statistics, which kRowLanes lanes a row join).
   for (int r = tid; r < S; r += kVerifyThreads) {
     const int up = r == 0 ? -1 : p.parents ? p.parents[(int64_t)b * S + r] : r - 1;
     const int x = r == 0 ? -1 : p.tokens[(int64_t)b * S + r];
@@ -271,8 +271,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
       chance[r] = tested && draft ? draft[up * p.qsr + x] : 0.0f;
     }
   }
-  for (int r0 = 0; r0 < S; r0 += kVerifyThreads / 16) {
-    const int r = r0 + (tid >> 4);
+  for (int r0 = 0; r0 < S; r0 += kVerifyThreads / kRowLanes) {
+    const int r = r0 + tid / kRowLanes, sub = tid % kRowLanes;
     const RowPart* parts = p.parts + ((int64_t)b * S + min(r, S - 1)) * p.row_slices;
     float t = -INFINITY;
     if constexpr (GREEDY) {
@@ -283,23 +283,24 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
           a = z;
         }
       };
-      for (int i = tid & 15; i < p.row_slices; i += 16) take(parts[i].top, parts[i].at);
+      for (int i = sub; i < p.row_slices; i += kRowLanes) take(parts[i].top, parts[i].at);
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) take(__shfl_xor(t, o), __shfl_xor(a, o));
-      if ((tid & 15) == 0 && r < S) best[r] = t > -INFINITY ? a : -1;
+      for (int o = kRowLanes / 2; o > 0; o >>= 1) take(__shfl_xor(t, o), __shfl_xor(a, o));
+      if (sub == 0 && r < S) best[r] = t > -INFINITY ? a : -1;
     } else {
       double s = 0.0;
-      for (int i = tid & 15; i < p.row_slices; i += 16) {
+#pragma unroll 4
+      for (int i = sub; i < p.row_slices; i += kRowLanes) {
         const RowPart part = parts[i];
         join(t, s, part.top, part.sum, p.k);
       }
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) {
+      for (int o = kRowLanes / 2; o > 0; o >>= 1) {
         const float y = __shfl_xor(t, o);
         const double z = __shfl_xor(s, o);
         join(t, s, y, z, p.k);
       }
-      if ((tid & 15) == 0 && r < S) {
+      if (sub == 0 && r < S) {
         top[r] = t;
         total[r] = t > -INFINITY ? s : __builtin_nan("");
       }
@@ -408,13 +409,19 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
   const int row = at_row;
   if (slice == 0) {
     // the accepted rows in order: ascending, as each comes after its parent
+    __shared__ uint64_t accepted[kMaxVerifyRows / 64];
+    for (int r = tid; r < kMaxVerifyRows; r += kVerifyThreads) {
+      const uint64_t mask = __ballot(r < S && taken[r]);
+      if (lane == 0) accepted[r >> 6] = mask;
+    }
+    __syncthreads();
     for (int r = tid; r < S; r += kVerifyThreads) {
-      int before = 0;
-      if (taken[r])
-        for (int y = 0; y < r; ++y) before += taken[y];
-      if (taken[r]) p.path[(int64_t)b * S + before] = r;
+      const bool in = accepted[r >> 6] >> (r & 63) & 1;
+      int place = __builtin_popcountll(accepted[r >> 6] & ((1ull << (r & 63)) - 1));
+      for (int y = 0; y < r >> 6; ++y) place += __builtin_popcountll(accepted[y]);
+      if (in) p.path[(int64_t)b * S + place] = r;
       if (r >= num_path) p.path[(int64_t)b * S + r] = -1;
-      if (p.row_weight) p.row_weight[(int64_t)b * S + r] = taken[r] ? 1.0f : 0.0f;
+      if (p.row_weight) p.row_weight[(int64_t)b * S + r] = in ? 1.0f : 0.0f;
     }
     if (tid == 0) p.count[b] = num_path;
   }
@@ -483,10 +490,17 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
       }
       return v;
     };
+    double first = 0.0, upto = 0.0;  // of the slices in the lanes: the first 64's are kept
     auto sum_all = [&] {
       double run = 0.0;
-      for (int s = 0; s < slices; s += 64)
-        run += __shfl(scan(s + lane < slices ? load_mass(s + lane) : 0.0), 63);
+      for (int s = 0; s < slices; s += 64) {
+        const double m = s + lane < slices ? load_mass(s + lane) : 0.0, incl = scan(m);
+        if (s == 0) {
+          first = m;
+          upto = incl;
+        }
+        run += __shfl(incl, 63);
+      }
       return run;
     };
     all = sum_all();
@@ -512,8 +526,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     int in = -1;
     double before = 0.0, run = 0.0;
     for (int s = 0; s < slices; s += 64) {
-      const double m = s + lane < slices ? load_mass(s + lane) : 0.0;
-      const double incl = run + scan(m);
+      const double m = s == 0 ? first : s + lane < slices ? load_mass(s + lane) : 0.0;
+      const double incl = s == 0 ? upto : run + scan(m);
       const uint64_t some = __ballot(m > 0.0), past = __ballot(m > 0.0 && incl > goal);
       const uint64_t from = past ? past & -past : some;
       if (from) {
@@ -551,9 +565,23 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
         mass_to += w[i][e];
         if (w[i][e] > 0.0 && mass_to > goal) found = min(found, (v0 + i) * VE - z.off + e);
       }
-    found = block_all(found, redi, [](int a, int d) { return min(a, d); });
+    // the first thread that found one (they are in the tokens' order), else the last of
+    // positive weight
+    const uint64_t any = __ballot(found != INT32_MAX), some = __ballot(final >= 0);
+    __shared__ int firsts[kVerifyThreads / 64], lasts[kVerifyThreads / 64];
+    const int f = any ? __builtin_amdgcn_readlane(found, __builtin_ctzll(any)) : INT32_MAX;
+    const int g = some ? __builtin_amdgcn_readlane(final, 63 - __builtin_clzll(some)) : -1;
+    if (lane == 0) {
+      firsts[tid >> 6] = f;
+      lasts[tid >> 6] = g;
+    }
     __syncthreads();
-    final = block_all(final, redi, [](int a, int d) { return max(a, d); });
+    found = firsts[0];
+    final = lasts[0];
+    for (int i = 1; i < kVerifyThreads / 64; ++i) {
+      found = min(found, firsts[i]);
+      final = max(final, lasts[i]);
+    }
     if (tid == 0) p.next[b] = found != INT32_MAX ? found : final;
   }
 }
