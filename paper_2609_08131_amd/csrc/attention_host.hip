@@ -148,6 +148,25 @@ jacap_status layout_weights(const AttnLaunch& A, bool bf16, WeightsSpace* w) {
   return sum_grid_ok(g, *w) ? JACAP_OK : JACAP_ERR_UNSUPPORTED;
 }
 
+// Of the chunks from `least` to twice it, the one whose rounds of a workgroup per compute unit
+// take the least: sequences end inside a chunk, half of one each on the average, so that chunks
+// of one round's tokens may be some workgroups more than one round (60 rows, four sequences
+// of 12001 to 16450 tokens, 8 KV heads: 1920 tokens are 272 workgroups, 62 us; 2048 are 248,
+// 52). A fiftieth over a round is taken as one: short chunks fill the gaps of empty ones.
+int round_chunk(const Geo& g, int least, int row_blocks) {
+  int best = least;
+  int64_t cost = INT64_MAX;
+  for (int64_t c = least; c <= 2 * (int64_t)least && c <= 1 << 20; c += 128) {
+    const int64_t blocks = (int64_t)g.L * g.H * row_blocks * (2 * g.T / c + g.B) / 2;
+    const int64_t rounds = std::max<int64_t>(1, (50 * blocks + 51 * kWideBlocks - 1) / (51 * kWideBlocks));
+    if (rounds * c < cost) {
+      cost = rounds * c;
+      best = (int)c;
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 jacap_status jacap::layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w, WeightsSpace* sum) {
@@ -167,6 +186,7 @@ jacap_status jacap::layout_attend(const AttnLaunch& A, bool bf16, AttendSpace* w
     const int64_t per = (LHT * w->row_blocks + kWideBlocks - 1) / kWideBlocks;
     w->chunk = (int)std::min<int64_t>(std::max<int64_t>((per + 127) / 128 * 128, kWideChunkMin),
                                       1 << 20);
+    if (A.at.row_mask) w->chunk = round_chunk(g, w->chunk, w->row_blocks);
     w->splits = std::max(1, (g.maxn + w->chunk - 1) / w->chunk);
     // Bounded by the tokens: with a place for each chunk of the longest in every sequence,
     // 64 sequences of which one has 131072 tokens would take 2 GB (252 rows, 8 KV heads;

@@ -1112,6 +1112,24 @@ def run_attn_weights_quant(prob: AttnWeightsQuantProblem, q, cache: QuantCache, 
                        prob.status, stream)
 
 
+def prepare_evict_quant_slots(cache: QuantCache, seq_offsets, seq_lens, budget: int, protect_last: int = 0,
+                              live_lens=None) -> EvictWeightedProblem:
+    """For run_evict_weighted_slots (which reads neither K nor V) over an 8-bit cache's
+    accumulators; seq_lens as prepare_quantize."""
+    quant = _quant_checks(seq_offsets, seq_lens, cache)
+    L, H, T, d = cache.k.shape
+    B, dev = len(seq_lens), cache.k.device
+    cfg = _quant_config(cache, torch.bfloat16, H, 1)
+    cfg.budget_k, cfg.protect_last = int(budget), int(protect_last)
+    row = torch.empty((B, L, H, 1, d), dtype=torch.bfloat16, device=dev)   # for its strides
+    batch = make_batch(seq_offsets, seq_lens, row, cache.k, cache.v)
+    attn = _attention(AttentionParams(live_lens=live_lens), B, 1, d, dev)
+    ws = _workspace(evict_weighted_workspace_size(cfg, batch, attn), dev)
+    layout = {"acc": _acc_layout(cache.k), "slots": (torch.Size((B, L, H)), torch.int32, dev)}
+    return EvictWeightedProblem(cfg, batch, attn, torch.empty((B, L, H, 0), dtype=torch.int32, device=dev), None,
+                                None, None, ws, live_lens, seq_offsets, layout)
+
+
 @dataclasses.dataclass
 class VerifyParams:
     """Parameters of verify (see jacap_verification in include/jacap.h)."""
