@@ -520,8 +520,8 @@ typedef struct jacap_quant {
  * all blocks that the sequences own (2^-100 where a block has no token).
  *   acc : optional float [L][H_kv][T_total] (dense): an empty slot (an entry below zero)
  *         has no token, its codes are kept as they are.
- * attn: live_lens is read. No workspace and no flags; num_q_heads and window are only
- * checked. k, v must not overlap the codes. */
+ * Of attn live_lens is read (its other fields, num_q_heads and window are checked as by
+ * jacap_attn_weights). No workspace and no flags. k, v must not overlap the codes. */
 jacap_status jacap_quantize(const jacap_config* cfg, const jacap_batch* batch,
                             const jacap_attention* attn, const jacap_quant* quant, const void* k,
                             const void* v, const float* acc, void* kq, void* vq, float* scales,
@@ -544,8 +544,9 @@ jacap_status jacap_quantize(const jacap_config* cfg, const jacap_batch* batch,
  *            clears it.
  * A token whose position is not one of its sequence's rows, whose place is past the slots or
  * whose row is not in 0 .. S-1 is not written and raises JACAP_FLAG_BAD_OFFSETS; of two
- * tokens for one position the later is written. attn's live_lens is not read. The cache,
- * scales and acc must not be written by others meanwhile. */
+ * tokens for one position the later is written. Of attn the dk and dv strides are read (its
+ * other fields are checked as by jacap_attend). The cache, scales and acc must not be written
+ * by others meanwhile. */
 jacap_status jacap_append_quant(const jacap_config* cfg, const jacap_batch* batch,
                                 const jacap_attention* attn, const jacap_quant* quant,
                                 const void* kd, const void* vd, const int32_t* start,

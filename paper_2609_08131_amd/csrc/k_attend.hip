@@ -641,16 +641,26 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   // forth may put blocks of several sequences here.
   const int item = blockIdx.x - rows_grid;
   const int lh = item / token_blocks, place = item - lh * token_blocks;
-  for (int b0 = 0; b0 < g.B; b0 += 64) {
-  const int lane = tid & 63;
-  const int2 held = b0 + lane < g.B ? sequence_rows(g, at, b0 + lane) : int2{0, -1};
-  const int first = (int)(min(max((int64_t)held.x, (int64_t)0), g.T) / kJoinTokens) + b0 + lane;
-  const int blocks = held.y < 0 ? 0 : max(1, (held.y + kJoinTokens - 1) / kJoinTokens);
-  uint64_t here = __ballot(place >= first && place < first + blocks);
-  for (; here; here &= here - 1) {
-  const int i = __builtin_ctzll(here), b = b0 + i, u = b * g.L * g.H + lh;
-  const Unit un = {b, lh / g.H, lh % g.H, 0, __builtin_amdgcn_readlane(held.x, i), __builtin_amdgcn_readlane(held.y, i)};
-  const int blk = place - __builtin_amdgcn_readlane(first, i), t0 = blk * kJoinTokens;
+  __shared__ uint64_t here[kThreads / 64];  // of the sequences b0 .., those with a block here
+  auto first_block = [&](int b, const int2& rows) {
+    return (int)(min(max((int64_t)rows.x, (int64_t)0), g.T) / kJoinTokens) + b;
+  };
+  for (int b0 = 0; b0 < g.B; b0 += kThreads) {
+  {
+    const int x = b0 + tid;
+    const int2 rows = x < g.B ? sequence_rows(g, at, x) : int2{0, -1};
+    const int first = first_block(x, rows);
+    const int blocks = rows.y < 0 ? 0 : max(1, (rows.y + kJoinTokens - 1) / kJoinTokens);
+    const uint64_t mask = __ballot(place >= first && place < first + blocks);
+    if ((tid & 63) == 0) here[tid >> 6] = mask;
+  }
+  __syncthreads();
+  for (int part = 0; part < kThreads / 64; ++part)
+  for (uint64_t todo = here[part]; todo; todo &= todo - 1) {
+  const int b = __builtin_amdgcn_readfirstlane(b0 + 64 * part + __builtin_ctzll(todo)), u = b * g.L * g.H + lh;
+  const int2 rows = sequence_rows(g, at, b);
+  const Unit un = {b, lh / g.H, lh % g.H, 0, __builtin_amdgcn_readfirstlane(rows.x), __builtin_amdgcn_readfirstlane(rows.y)};
+  const int blk = place - first_block(b, rows), t0 = blk * kJoinTokens;
   // The entries and the rows' logits are requested before the rows' lse is joined.
   // Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
   const int64_t tr = token_row(g, un) + t0;
@@ -727,6 +737,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
   }
   __syncthreads();  // the rows' lse is read before another block's is written
   }
+  __syncthreads();
   }
 }
 

@@ -583,6 +583,77 @@ def test_streams_and_repeats(jacap):
         check_attend(c, p, None, False, False)
 
 
+@pytest.mark.parametrize("dtype,S,G", [(BF, 1, 4), (F32, 5, 2), (BF, 40, 2)])
+def test_no_cached_tokens_at_all(jacap, dtype, S, G):
+    """A cache of no rows: attention of the drafted tokens among themselves."""
+    c = Case([0, 0], S, dtype, 64, H=2, G=G, seed=2)
+    cache = jacap.alloc_quant_cache(1, 2, 0, 64)
+    for accumulate in (False, True):
+        p = jacap.AttentionParams(accumulate=accumulate)
+        prob = jacap.prepare_attend_quant(c.q, cache, c.kd, c.vd, c.offsets, [0, 0], p)
+        acc = torch.zeros((1, 2, 0), device="cuda")
+        jacap.run_attend_quant(prob, c.q, cache, c.kd, c.vd, acc=acc)
+        assert jacap.read_status(prob.ws) == 0
+        c.acc, c.live = acc, None
+        check_attend(c, prob, acc, False, accumulate)
+    wp = jacap.prepare_attn_weights_quant(c.q, cache, c.offsets, [0, 0], p)
+    jacap.run_attn_weights_quant(wp, c.q, cache, acc, prob.lse)
+    k = torch.empty((1, 2, 0, 64), dtype=dtype, device="cuda")
+    jacap.run_quantize(jacap.prepare_quantize(k, k, cache, c.offsets, [0, 0]), k, k, cache)
+    ap = jacap.prepare_append_quant(c.kd, c.vd, cache, c.offsets, [0, 0])
+    jacap.run_append_quant(ap, c.kd, c.vd, cache, start=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert int(ap.status) == jacap.FLAG_BAD_OFFSETS      # there is no room
+
+
+def test_offsets_past_32_bits(jacap):
+    """Codes and drafted rows more than 2^32 bytes apart: a cache of 34 M rows of one head (4.4
+    GB each of K and V), two sequences at its ends, the rows between them reserved."""
+    T, d = 34 * (1 << 20), 128
+    ends = [200, 333]
+    cache = jacap.QuantCache(torch.empty((1, 1, T, d), dtype=E4, device="cuda"),
+                             torch.empty((1, 1, T, d), dtype=E4, device="cuda"),
+                             torch.full((1, 1, T // 32, 2), 2.0 ** -100, device="cuda"), 32)
+    rows = [T - 512, 512]
+    off = torch.tensor([0, T - 512, T], dtype=torch.int32, device="cuda")
+    live = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    c = Case(ends, 3, BF, d, H=1, G=2, seed=31)
+    S = 3
+    # the tokens are appended, some at a time, to where each sequence begins
+    start = torch.zeros(2, dtype=torch.int32, device="cuda")
+    kd, vd = torch.zeros((2, 1, 1, 333, d), dtype=BF, device="cuda"), torch.zeros((2, 1, 1, 333, d), dtype=BF, device="cuda")
+    for b, n in enumerate(ends):
+        sl = slice(c.starts[b], c.starts[b] + n)
+        kd[b, 0, 0, :n], vd[b, 0, 0, :n] = c.k[0, 0, sl], c.v[0, 0, sl]
+    ap = jacap.prepare_append_quant(kd, vd, cache, off, rows)
+    jacap.run_append_quant(ap, kd, vd, cache, start=start, count=live, start_out=start)
+    assert start.tolist() == ends and int(ap.status) == 0
+    for b, n in enumerate(ends):
+        lo = int(off[b])
+        for x, codes, i in ((c.k, cache.k, 0), (c.v, cache.v, 1)):
+            rowsn = up_to(n, 32)
+            fine = cache.scales[0, 0, lo // 32:(lo + rowsn) // 32, i].repeat_interleave(32)[:n, None]
+            got = codes[0, 0, lo:lo + n].float() * fine
+            ref = x[0, 0, c.starts[b]:c.starts[b] + n]
+            assert bool(((got - ref.float()).abs() <= torch.maximum(ref.float().abs() / 16, fine / 1024)).all())
+            ref.copy_(got.to(BF))
+    prob = jacap.prepare_attend_quant(c.q, cache, c.kd, c.vd, off, rows, jacap.AttentionParams(live_lens=live))
+    jacap.run_attend_quant(prob, c.q, cache, c.kd, c.vd)
+    c.live = None
+    check_attend(c, prob, None, False, False)
+
+
+@pytest.mark.parametrize("B", [300, 700])
+def test_many_sequences_that_accumulate(jacap, B):
+    """More sequences than a workgroup has threads: each finds the blocks of its tokens."""
+    gen = torch.Generator().manual_seed(B)
+    lens = [int(x) for x in torch.randint(0, 40, (B,), generator=gen)]
+    lens[17], lens[B - 2] = 2500, 1100
+    c = QuantCase(jacap, lens, 1, BF, 64, 16, 1, H=1, G=2, holes=0.1, seed=B)
+    prob, acc = run_attend(jacap, c, True, True, decay=0.5)
+    check_attend(c, prob, acc, True, True, decay=0.5)
+
+
 def test_refusals(jacap):
     c = QuantCase(jacap, [100, 20], 3, BF, 64, 32, H=2, G=2, seed=1)
     p = jacap.AttentionParams(live_lens=c.live)
