@@ -24,6 +24,8 @@ constexpr int kMaxDraft = 512;        // rows per query head jacap_attend takes
 constexpr int kKeepRows = 16;
 constexpr int kSpans = 512;           // workgroups the attention of few rows is cut into, of
 constexpr int kSpanMin = 256;         // ... at least this many tokens
+// Tokens up to which a workgroup takes a whole unit of an 8-bit cache, and none joins pieces.
+constexpr int kWholeTokens = 512;
 constexpr int kUnitGroups = 4;        // what beginning and ending a unit costs, in groups of 4 steps
 constexpr int64_t kMaxGroups = INT32_MAX / 2;  // groups of a batch
 constexpr int kWideChunkMin = 256;    // tokens per workgroup of many rows, at least
@@ -197,6 +199,7 @@ struct AttendSpace {
   size_t zd;           // float  [U][R][S]          ... and the drafted tokens'
   size_t total;
   bool keep;           // logits are kept
+  bool whole = false;  // a workgroup per unit and row block: no spans, no pieces
 };
 
 struct WeightsSpace {

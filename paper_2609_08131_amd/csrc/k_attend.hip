@@ -750,13 +750,14 @@ static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, int grou
                 ws_ptr<int32_t>(ws, w.before), w.keep ? ws_ptr<float>(ws, w.z) : nullptr,
                 w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, acc, acc_draft};
   const bool wide = w.rw > 0;
-  const JoinGeo jg{w.chunk, w.places, wide ? 0 : w.spans, group, 16 * w.mt, w.row_blocks};
+  const JoinGeo jg{w.whole ? INT32_MAX / 2 : w.chunk, w.places, wide || w.whole ? 0 : w.spans, group, 16 * w.mt,
+                   w.row_blocks};
   // Spans of a batch of many rows hold many units each, so a row has few pieces; of
   // few rows (at most a workgroup's worth per compute unit), as many as there are spans.
   const int64_t UR = (int64_t)g.U * A.at.R;
   const int few = wide ? w.splits <= kJoinFew : UR > kJoinRows;
   const int64_t per = few ? kThreads / (D / 4) : 1;
-  const int rows_grid = wide && w.splits == 1 ? 0 : (int)((UR + per - 1) / per);
+  const int rows_grid = w.whole || (wide && w.splits == 1) ? 0 : (int)((UR + per - 1) / per);
   const int token_blocks = (int)(g.T / kJoinTokens) + g.B;  // of a (layer, KV head)
   const int64_t grid = rows_grid + (w.keep ? (int64_t)g.L * g.H * token_blocks : 0);
   auto go = [&](auto kern) {

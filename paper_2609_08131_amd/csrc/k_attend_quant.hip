@@ -93,6 +93,7 @@ struct QuantParams {
   AttendArgs<T> p;
   QuantArgs qa;
   int row_blocks;
+  int whole;  // a workgroup per unit and row block
 };
 
 // 16-token tiles of a step.
@@ -118,15 +119,24 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
   int2 held = rows64(0);
   int held_b = 0;
   int64_t seq_groups = 0;
+  int b = 0, before = 0;  // the sequence of the span's first group, and the groups before it
+  int at_group, end_group, quantum = 1, total = 0;
+  if (params.whole) {
+    // as if the sequence were the first one
+    b = blockIdx.x / per_seq;
+    held = rows64(held_b = b & ~63);
+    const int c = real_groups(__builtin_amdgcn_readlane(held.y, b - held_b), GROUP);
+    at_group = (blockIdx.x - b * per_seq) * (c + kUnitGroups);
+    end_group = at_group + c;
+  } else {
   for (int b0 = 0; b0 < B; b0 += 64)
     seq_groups += (uint32_t)__builtin_amdgcn_readlane(wave_scan(groups64(b0 == 0 ? held : rows64(b0))), 63);
   // (more than the host allowed for: offsets that go back and forth, flagged; no work)
-  const int total = seq_groups * per_seq <= kMaxGroups ? (int)(seq_groups * per_seq) : 0;
-  const int quantum = span_quantum(total, gridDim.x, GROUP);
-  int at_group = blockIdx.x * quantum;
-  const int end_group = min(total, at_group + quantum);
-  // the sequence of the span's first group, and the groups before it (of one unit each)
-  int b = 0, before = 0;
+  total = seq_groups * per_seq <= kMaxGroups ? (int)(seq_groups * per_seq) : 0;
+  quantum = span_quantum(total, gridDim.x, GROUP);
+  at_group = blockIdx.x * quantum;
+  end_group = min(total, at_group + quantum);
+  // (the groups before it are of one unit each)
   for (int b0 = 0; b0 < B; b0 += 64) {
     if (b0 > 0) held = rows64(held_b = b0);
     const int c = groups64(held), incl = before + wave_scan(c);
@@ -138,6 +148,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
       break;
     }
     before = __builtin_amdgcn_readlane(incl, 63);
+  }
   }
   while (at_group < end_group) {
   // The parameters are read again for each unit, as attend_kernel reads them.
@@ -776,7 +787,8 @@ static hipError_t attend_quant_typed(const QuantLaunch& Q, const AttendSpace& w,
                   w.keep ? ws_ptr<float>(ws, w.zd) : nullptr, ws_ptr<uint32_t>(ws, 0),
                   ws_ptr<int32_t>(ws, w.before)};
   auto go = [&](auto kern) {
-    kern<<<w.spans, kThreads, 0, A.base.stream>>>(QuantParams<T>{g, A.at, p, Q.q, w.row_blocks});
+    const unsigned grid = w.whole ? (unsigned)(g.U * w.row_blocks) : w.spans;
+    kern<<<grid, kThreads, 0, A.base.stream>>>(QuantParams<T>{g, A.at, p, Q.q, w.row_blocks, w.whole});
   };
   if constexpr (sizeof(T) == 2) {
     if (w.rw > 0) {

@@ -129,7 +129,8 @@ static void run(const Shape& s) {
     }
     if (w.keep) EXPECT(w.zd >= w.z + 64 * (size_t)s.L * s.H * (size_t)(s.total / 16 + s.B + 1) * R);
     EXPECT(summed == (accumulate && !w.keep && s.total > 0));
-    EXPECT(joined == (w.rw == 0 || w.splits > 1));
+    EXPECT(joined == (w.whole ? w.keep : w.rw == 0 || w.splits > 1));
+    EXPECT(!w.whole || (n <= 512 && w.rw == 0));
   }
   a.accumulate = 0;
   quantized = appended = summed = 0;
