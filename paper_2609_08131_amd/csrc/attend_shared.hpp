@@ -75,7 +75,7 @@ __device__ __forceinline__ int2 sequence_rows(const Geo& g, const Attn& at, int 
   const int32_t a = g.seq_off[b], e = g.seq_off[b + 1];
   int n = offsets_ok(g, a, e) ? e - a : 0;
   if (g.live) n = live_ok(g, b, n) ? g.live[b] : 0;
-  if (!whole_blocks(g, at, b)) n = 0;
+  if ((a | e) & at.row_mask) n = 0;  // as whole_blocks
   return int2{a, n};
 }
 // Inclusive scan over the wave's lanes.

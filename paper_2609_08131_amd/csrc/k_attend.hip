@@ -567,8 +567,9 @@ __device__ __forceinline__ Pieces pieces_of(const Geo& g, const JoinGeo& j, cons
   return {(start + c - 1) / q - start / q + 1, start, q, j.rows, r % j.rows};
 }
 
-// ROWS: at least the rows whose logits are kept.
-template <typename T, int D, int ROWS>
+// ROWS: at least the rows whose logits are kept. APART: the sequences' lengths lie so far
+// apart that the accumulators' blocks are those of the tokens there are.
+template <typename T, int D, int ROWS, bool APART>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, JoinArgs<T> p,
                                                                JoinGeo jg, int few, int rows_grid,
                                                                int token_blocks) {
@@ -634,33 +635,10 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     }
     return;
   }
-  // The blocks of a (layer, KV head) are its sequences' side by side, as they lie in the
-  // cache: sequence b's begin behind seq_off[b] / kJoinTokens + b others, which is room for
-  // the last, partial one of each. (A block for each of the longest in every sequence: 8 units
-  // of 131072 tokens beside 56 of 31 to 32768, 21 us, 14.6 so.) Offsets that go back and
-  // forth may put blocks of several sequences here.
   const int item = blockIdx.x - rows_grid;
-  const int lh = item / token_blocks, place = item - lh * token_blocks;
-  __shared__ uint64_t here[kThreads / 64];  // of the sequences b0 .., those with a block here
-  auto first_block = [&](int b, const int2& rows) {
-    return (int)(min(max((int64_t)rows.x, (int64_t)0), g.T) / kJoinTokens) + b;
-  };
-  for (int b0 = 0; b0 < g.B; b0 += kThreads) {
-  {
-    const int x = b0 + tid;
-    const int2 rows = x < g.B ? sequence_rows(g, at, x) : int2{0, -1};
-    const int first = first_block(x, rows);
-    const int blocks = rows.y < 0 ? 0 : max(1, (rows.y + kJoinTokens - 1) / kJoinTokens);
-    const uint64_t mask = __ballot(place >= first && place < first + blocks);
-    if ((tid & 63) == 0) here[tid >> 6] = mask;
-  }
-  __syncthreads();
-  for (int part = 0; part < kThreads / 64; ++part)
-  for (uint64_t todo = here[part]; todo; todo &= todo - 1) {
-  const int b = __builtin_amdgcn_readfirstlane(b0 + 64 * part + __builtin_ctzll(todo)), u = b * g.L * g.H + lh;
-  const int2 rows = sequence_rows(g, at, b);
-  const Unit un = {b, lh / g.H, lh % g.H, 0, __builtin_amdgcn_readfirstlane(rows.x), __builtin_amdgcn_readfirstlane(rows.y)};
-  const int blk = place - first_block(b, rows), t0 = blk * kJoinTokens;
+  __shared__ float slse[kKeepRows], sw[kKeepRows];
+  auto accumulate = [&](const Unit& un, int u, int blk) {
+  const int t0 = blk * kJoinTokens;
   // The entries and the rows' logits are requested before the rows' lse is joined.
   // Token t0 + tid + 256 x: entry tid % 16 of tile (t0 + tid) / 16 + 16 x.
   const int64_t tr = token_row(g, un) + t0;
@@ -679,7 +657,6 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
     for (int r = 0; r < ROWS; ++r)
       if (r < R) y[r][x] = logit(r, x);
   }
-  __shared__ float slse[kKeepRows], sw[kKeepRows];
   {
     // 16 threads per row; a row of one piece has its lse already, as a sum of 1
     const int r = tid >> 4, rc = min(r, R - 1);
@@ -735,9 +712,40 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(Geo g, Attn at, J
         sum = __builtin_fmaf(sw[r], exp2_fast(p.zd[((int64_t)u * R + r) * S + tid] - slse[r]), sum);
     p.acc_draft[(int64_t)u * S + tid] = sum;
   }
-  __syncthreads();  // the rows' lse is read before another block's is written
-  }
-  __syncthreads();
+  };
+  if constexpr (!APART) {
+    const int u = item / token_blocks, blk = item - u * token_blocks;
+    const Unit un = attention_unit(g, at, u);
+    if (blk * kJoinTokens < un.n || blk == 0) accumulate(un, u, blk);
+  } else {
+    // The blocks of a (layer, KV head) are its sequences' side by side, as they lie in the
+    // cache: sequence b's begin behind seq_off[b] / kJoinTokens + b others, which is room for
+    // the last, partial one of each. Offsets that go back and forth may put blocks of several
+    // sequences here.
+    const int lh = item / token_blocks, place = item - lh * token_blocks;
+    __shared__ uint64_t here[kThreads / 64];  // of the sequences b0 .., those with a block here
+    auto first_block = [&](int b, const int2& rows) {
+      return (int)(min(max((int64_t)rows.x, (int64_t)0), g.T) / kJoinTokens) + b;
+    };
+    for (int b0 = 0; b0 < g.B; b0 += kThreads) {
+      const int x = b0 + tid;
+      const int2 rows = x < g.B ? sequence_rows(g, at, x) : int2{0, -1};
+      const int first = first_block(x, rows);
+      const int blocks = rows.y < 0 ? 0 : max(1, (rows.y + kJoinTokens - 1) / kJoinTokens);
+      const uint64_t mask = __ballot(place >= first && place < first + blocks);
+      if ((tid & 63) == 0) here[tid >> 6] = mask;
+      __syncthreads();
+      for (int part = 0; part < kThreads / 64; ++part)
+        for (uint64_t todo = here[part]; todo; todo &= todo - 1) {
+          const int b = __builtin_amdgcn_readfirstlane(b0 + 64 * part + __builtin_ctzll(todo));
+          const int2 rows = sequence_rows(g, at, b);
+          const Unit un = {b, lh / g.H, lh % g.H, 0, __builtin_amdgcn_readfirstlane(rows.x),
+                           __builtin_amdgcn_readfirstlane(rows.y)};
+          accumulate(un, b * g.L * g.H + lh, place - first_block(b, rows));
+          __syncthreads();  // the rows' lse is read before another block's is written
+        }
+      __syncthreads();
+    }
   }
 }
 
@@ -758,13 +766,20 @@ static hipError_t join_typed(const AttnLaunch& A, const AttendSpace& w, int grou
   const int few = wide ? w.splits <= kJoinFew : UR > kJoinRows;
   const int64_t per = few ? kThreads / (D / 4) : 1;
   const int rows_grid = w.whole || (wide && w.splits == 1) ? 0 : (int)((UR + per - 1) / per);
-  const int token_blocks = (int)(g.T / kJoinTokens) + g.B;  // of a (layer, KV head)
-  const int64_t grid = rows_grid + (w.keep ? (int64_t)g.L * g.H * token_blocks : 0);
+  // A workgroup that finds its unit without tokens there costs little while others work, the
+  // look for a block's sequence 1 us (a block for each of the longest, or those there are:
+  // 32 units of 131072 tokens 9.6 us, 10.8; 128 units of 4096 to 32768, about 2000 workgroups
+  // more, 15.1, 16.0; 8 units of 131072 beside 56 of 31 to 32768, 7000 more, 21.2, 14.6).
+  const int unit_blocks = std::max(1, (g.maxn + kJoinTokens - 1) / kJoinTokens);
+  const int head_blocks = (int)(g.T / kJoinTokens) + g.B;  // of a (layer, KV head)
+  const bool apart = w.keep && (int64_t)g.L * g.H * ((int64_t)g.B * unit_blocks - head_blocks) > 4096;
+  const int token_blocks = apart ? head_blocks : unit_blocks;
+  const int64_t grid = rows_grid + (w.keep ? (int64_t)g.L * g.H * (apart ? 1 : g.B) * token_blocks : 0);
   auto go = [&](auto kern) {
     kern<<<(unsigned)grid, kThreads, 0, A.base.stream>>>(g, A.at, p, jg, few, rows_grid, token_blocks);
   };
-  if (!w.keep || A.at.R <= 4) go(attend_join_kernel<T, D, 4>);
-  else go(attend_join_kernel<T, D, kKeepRows>);
+  if (!w.keep || A.at.R <= 4) apart ? go(attend_join_kernel<T, D, 4, true>) : go(attend_join_kernel<T, D, 4, false>);
+  else apart ? go(attend_join_kernel<T, D, kKeepRows, true>) : go(attend_join_kernel<T, D, kKeepRows, false>);
   return hipGetLastError();
 }
 

@@ -12,6 +12,7 @@ import math
 import pytest
 import torch
 
+import test_gpu_attention
 from attention_ref import U, Weights, check, half_step, sees_tree
 from quant_ref import codes_of, quantize, scale_exponent
 from test_gpu_attention import BF, F32, Case
@@ -652,6 +653,24 @@ def test_many_sequences_that_accumulate(jacap, B):
     c = QuantCase(jacap, lens, 1, BF, 64, 16, 1, H=1, G=2, holes=0.1, seed=B)
     prob, acc = run_attend(jacap, c, True, True, decay=0.5)
     check_attend(c, prob, acc, True, True, decay=0.5)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_accumulation_at_lengths_far_apart(jacap, wide):
+    """A long sequence among short and empty ones, with slots that are not full: the weights are
+    joined by blocks of the tokens there are."""
+    gen = torch.Generator().manual_seed(3)
+    lens = [int(x) for x in torch.randint(0, 40, (300,), generator=gen)]
+    lens[17], lens[280], lens[299] = 20000, 1100, 0
+    kw = dict(H=1, G=2, holes=0.1, seed=5)
+    if wide:
+        c = Case(lens, 1, BF, 64, spare=7, **kw)
+        prob, acc = test_gpu_attention.run_attend(jacap, c, True, True, decay=0.5)
+        test_gpu_attention.check_attend(c, prob, acc, True, True, decay=0.5)
+    else:
+        c = QuantCase(jacap, lens, 1, BF, 64, 16, 1, **kw)
+        prob, acc = run_attend(jacap, c, True, True, decay=0.5)
+        check_attend(c, prob, acc, True, True, decay=0.5)
 
 
 def test_refusals(jacap):
