@@ -597,7 +597,8 @@ jacap_status jacap_attn_weights_quant(const jacap_config* cfg, const jacap_batch
  * where there is none; p's where rounding leaves nothing of w).
  * temperature = 0 (greedy): the child whose token is the row's largest logit (the first of
  * equal ones) is accepted, and the last row's largest is next; uniform and draft are not
- * read. Sums over the vocabulary are fp64, exponentials fp32.
+ * read. Exponentials are fp32; sums over the vocabulary fp64 (of a row's total: of the fp32
+ * sums of 4 or 8 neighbours).
  *
  * Rows whose parent is not one of 0 .. r-1 (-1: padding) and tokens outside 0 .. vocab-1 are
  * not tested. A current row with a NaN or +inf logit, or of only -inf (greedy: without a

@@ -673,6 +673,48 @@ def test_accumulation_at_lengths_far_apart(jacap, wide):
         check_attend(c, prob, acc, True, True, decay=0.5)
 
 
+def test_another_device_is_refused(jacap, monkeypatch):
+    """A run with another device current, or on another device's stream, enqueues nothing."""
+    c = QuantCase(jacap, [50, 20], 3, BF, 64, 32, H=2, G=2, seed=26)
+    p = jacap.AttentionParams(accumulate=True, live_lens=c.live)
+    prob = jacap.prepare_attend_quant(c.q, c.cache, c.kd, c.vd, c.offsets, c.rows, p)
+    wp = jacap.prepare_attn_weights_quant(c.q, c.cache, c.offsets, c.rows, p)
+    qp = jacap.prepare_quantize(c.k, c.v, c.cache, c.offsets, c.rows, live_lens=c.live)
+    ap = jacap.prepare_append_quant(c.kd, c.vd, c.cache, c.offsets, c.rows)
+    logits = torch.randn((2, 3, 50), device="cuda")
+    tokens = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    vp = jacap.prepare_verify(logits, jacap.VerifyParams(temperature=0.0))
+    acc, start = c.acc.clone(), c.live.clone()
+    held = [x.view(torch.uint8).clone() for x in (c.cache.k, c.cache.v, c.cache.scales)]
+    for x in (prob.out, vp.next):
+        x.fill_(7)
+
+    class Elsewhere:
+        device_index, cuda_stream = 1, 0
+
+    def refused(stream):
+        for run in (lambda: jacap.run_attend_quant(prob, c.q, c.cache, c.kd, c.vd, acc=acc, stream=stream),
+                    lambda: jacap.run_attn_weights_quant(wp, c.q, c.cache, acc, prob.lse, stream=stream),
+                    lambda: jacap.run_quantize(qp, c.k, c.v, c.cache, stream=stream),
+                    lambda: jacap.run_append_quant(ap, c.kd, c.vd, c.cache, start=start, stream=stream),
+                    lambda: jacap.run_verify(vp, logits, tokens, stream=stream)):
+            with pytest.raises(ValueError):
+                run()
+
+    refused(Elsewhere)
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        refused(None)
+    torch.cuda.synchronize()
+    assert torch.equal(acc, c.acc) and bool((prob.out == 7).all()) and bool((vp.next == 7).all())
+    for x, y in zip((c.cache.k, c.cache.v, c.cache.scales), held):
+        assert torch.equal(x.view(torch.uint8), y)
+    side = torch.cuda.Stream()
+    jacap.run_attend_quant(prob, c.q, c.cache, c.kd, c.vd, acc=acc, stream=side)
+    torch.cuda.synchronize()
+    check_attend(c, prob, acc, True, True)
+
+
 def test_refusals(jacap):
     c = QuantCase(jacap, [100, 20], 3, BF, 64, 32, H=2, G=2, seed=1)
     p = jacap.AttentionParams(live_lens=c.live)
