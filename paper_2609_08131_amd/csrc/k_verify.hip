@@ -472,6 +472,15 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     };
     __shared__ int last;
     double* mass = p.mass + (int64_t)b * slices;
+    // (known from the row's sum: at a rejected token, whose weight is left out above, it would
+    // not be seen below)
+    if (!(total[row] < INFINITY)) {  // a NaN or an infinity, or -inf only: not a row to draw from
+      if (slice == 0 && tid == 0) {
+        p.next[b] = -1;
+        atomicOr(p.status, (uint32_t)JACAP_FLAG_NONFINITE);
+      }
+      return;
+    }
     const double mine = slice_sum(slice, c);
     if (tid == 0) {
       __hip_atomic_store(&mass[slice], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -519,7 +528,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
       __syncthreads();
       all = sum_all();
     }
-    if (!(all > 0.0) || !(all < INFINITY)) {  // not a row to draw from
+    if (!(all > 0.0) || !(all < INFINITY)) {  // draft probabilities to draw by that are not numbers
       if (tid == 0) {
         p.next[b] = -1;
         atomicOr(p.status, (uint32_t)JACAP_FLAG_NONFINITE);
