@@ -598,7 +598,8 @@ jacap_status jacap_attn_weights_quant(const jacap_config* cfg, const jacap_batch
  * temperature = 0 (greedy): the child whose token is the row's largest logit (the first of
  * equal ones) is accepted, and the last row's largest is next; uniform and draft are not
  * read. Exponentials are fp32; sums over the vocabulary fp64 (of a row's total: of the fp32
- * sums of 4 or 8 neighbours).
+ * sums of 4 or 8 neighbours; a test without draft probabilities that this could turn is made with
+ * the fp64 sum of what is left).
  *
  * Rows whose parent is not one of 0 .. r-1 (-1: padding) and tokens outside 0 .. vocab-1 are
  * not tested. A current row with a NaN or +inf logit, or of only -inf (greedy: without a

@@ -9,7 +9,7 @@
 // last joins the slices' sums and finds the token in one of them. Every slice's workgroup walks
 // for itself: it costs less than a launch.
 //
-// (16 trees of 64 rows: 15 us; 31 before lanes shared a row's parts and the draw's place.)
+// (16 trees of 64 rows: 16.5 us; 31 before lanes shared a row's parts and the draw's place.)
 //
 // The draw's sums are fp64: the exponentials have 24 bits, and the draw's border must not move
 // with the order in which 128256 of them are added. A row's total is fp64 too, of the
@@ -24,6 +24,15 @@ namespace {
 
 constexpr int kSliceVecs = kVerifyThreads * kVerifyVecs;
 constexpr int kRowLanes = 4;  // that join the parts of a row
+
+// How far a row's total may be from the sum of the weights that the draw uses, relative to it.
+// Of a weight 2^-a (at most 1, the largest's): a pair's fp32 additions 3 x 2^-24; two exponents
+// of about a, each the product of a rounded difference, 4 a 2^-24; the joins of up to 2048 slices
+// by four lanes, 2^-23 for each that raises the maximum, at most 520 in a row. The weights' mean
+// of a is at most log2 V <= 24, so all are below (3 + 96 + 1040) 2^-24 < 2^-13.
+constexpr double kTotalError = 0x1p-13;
+// ... and of the sum of at most 2^24 weights by 256 threads in fp64: 2^16 + 10 additions in a row.
+constexpr double kSumError = 0x1p-36;
 
 // A row of V logits as 16-byte pieces: piece v holds elements v VE - off .., off that of the
 // row's first in its own. lo .. hi are the pieces inside the row.
@@ -324,13 +333,39 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     if (tid == 0) left = total[0];
     __syncthreads();
   }
-  // One sweep over the rows in order meets every child of an accepted row after it.
-  for (;;) {
+  // The weights max(e - mul q, 0) of pieces v0, v0 + step ... of a row z of largest logit t (0
+  // outside it), those of the first n_gone rejected tokens 0.
+  auto weights = [&](const Row& z, const float* q, float t, double mul, int n_gone, int v0, int step,
+                     double (&w)[kVerifyVecs][VE]) __attribute__((always_inline)) {
+    float x[kVerifyVecs][VE], y[kVerifyVecs][VE];
+    z.load(v0, step, x);
+    if (mul != 0.0) z.load_draft(q, v0, step, y);
+    uint32_t out = 0;  // bit VE i + e: a rejected token
+    for (int g = 0; g < n_gone; ++g) {
+      const int x = token[gone[g]] + z.off, v = x / VE - v0;
+      if (v >= 0 && v % step == 0 && v / step < kVerifyVecs) out |= 1u << (v / step * VE + x % VE);
+    }
+#pragma unroll
+    for (int i = 0; i < kVerifyVecs; ++i)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        w[i][e] = (double)(out >> (VE * i + e) & 1 ? 0.0f : expo(x[i][e], t, p.k));
+        if (mul != 0.0) w[i][e] = rest(w[i][e], mul, (double)y[i][e]);
+      }
+  };
+  // One sweep over the rows in order meets every child of an accepted row after it. Without draft
+  // probabilities N is the row's total less the rejected tokens' weights, which may be wrong by as
+  // much as the total is: a test that this could turn is made with the sum of the weights
+  // themselves, which a last child that has all that is left needs (16 trees of 64 rows: 16.5
+  // us, 15.5 without).
+  for (bool summed = false;; summed = true) {  // summed: N is that sum, for the first test
     if (tid < 64) {
-      // (every lane has the same values, and stores them)
+      // (every lane has the same values, and stores them; the ballots tell the compiler so)
       int row = at_row, n_gone = num_gone, n_path = num_path, r = at_next;
       double c = mult, n = GREEDY ? 0.0 : left;
       bool stale = false, stop = false;  // N is not that of the weights
+      bool fresh = summed;
+      double slack = GREEDY ? 0.0 : summed ? n * kSumError : n * kTotalError;  // N is known to
       for (int r0 = r & ~63; r0 < S && !stop; r0 += 64) {
         const int up = r0 + lane < S ? parent[r0 + lane] : -1;
         uint64_t todo = __ballot(up == row) & (r > r0 ? ~0ull << (r - r0) : ~0ull);
@@ -349,7 +384,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
             const double u = (double)uniform[r], e = (double)weight[r];
             if (draft) {
               const double q = (double)chance[r];
-              accept = u * q * n < rest(e, c, q);
+              accept = __ballot(u * q * n < rest(e, c, q)) != 0;
               if (!accept) {
                 c += n;
                 stale = true;
@@ -357,11 +392,17 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
             } else {
               bool again = false;  // the token of a sibling already rejected
               for (int y = lane; y < n_gone; y += 64) again |= token[gone[y]] == token[r];
-              again = __ballot(again) != 0;
-              accept = !again && u * n < e;
+              again = __ballot(again) != 0 || e == 0.0;
+              const double past = u * n - e, far = fresh ? 0.0 : slack;
+              accept = __ballot(!again && past < -far) != 0;
+              if (!accept && __ballot(!again && past <= far && far > 0.0) != 0) {
+                stop = true;
+                break;
+              }
               if (!accept && !again) {
                 gone[n_gone++] = (int16_t)r;
                 n = rest(n, 1.0, e);
+                fresh = false;
               }
             }
           }
@@ -372,7 +413,11 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
             n_gone = 0;
             c = 0.0;
             stale = false;
-            if (!GREEDY) n = total[row];
+            fresh = false;
+            if (!GREEDY) {
+              n = total[row];
+              slack = n * kTotalError;
+            }
             todo = __ballot(up == row) & (i == 63 ? 0ull : ~0ull << (i + 1));
           }
         }
@@ -389,21 +434,21 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     }
     __syncthreads();
     if (at_next >= S) break;
-    // N = sum of max(e - C q, 0) over the current row, by the whole workgroup
+    // N by the whole workgroup
     if constexpr (!GREEDY) {
-      const int row = at_row;
+      const int row = at_row, n_gone = num_gone;
       const double c = mult;
       const Row z(logits + row * p.lsr, p.V);
-      const float* q = draft + row * p.qsr;
+      const float* q = draft ? draft + row * p.qsr : nullptr;
+      const float t = top[row];
       double sum = 0.0;
       for (int v = tid; v < z.pieces; v += kVerifyThreads * kVerifyVecs) {
-        float x[kVerifyVecs][VE], y[kVerifyVecs][VE];
-        z.load(v, kVerifyThreads, x);
-        z.load_draft(q, v, kVerifyThreads, y);
+        double w[kVerifyVecs][VE];
+        weights(z, q, t, c, n_gone, v, kVerifyThreads, w);
 #pragma unroll
         for (int i = 0; i < kVerifyVecs; ++i)
 #pragma unroll
-          for (int e = 0; e < VE; ++e) sum += rest((double)expo(x[i][e], top[row], p.k), c, (double)y[i][e]);
+          for (int e = 0; e < VE; ++e) sum += w[i][e];
       }
       sum = block_all(sum, redd, [](double a, double d) { return a + d; });
       if (tid == 0) left = sum;
@@ -439,31 +484,10 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     const float* q = draft ? draft + row * p.qsr : nullptr;
     const float t = top[row];
     const double c = mult;
-    const int n_gone = num_gone;
-    // The weights of pieces v0, v0 + step ... (0 outside the row), less the rejected tokens'.
-    auto weights = [&](int v0, int step, double mul, double (&w)[kVerifyVecs][VE]) __attribute__((always_inline)) {
-      float x[kVerifyVecs][VE], y[kVerifyVecs][VE];
-      z.load(v0, step, x);
-      if (mul != 0.0) z.load_draft(q, v0, step, y);
-#pragma unroll
-      for (int i = 0; i < kVerifyVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          w[i][e] = (double)expo(x[i][e], t, p.k);
-          if (mul != 0.0) w[i][e] = rest(w[i][e], mul, (double)y[i][e]);
-        }
-      for (int g = 0; g < n_gone; ++g) {
-        const int x = token[gone[g]] + z.off, v = x / VE - v0;
-        if (v < 0 || v % step != 0 || v / step >= kVerifyVecs) continue;
-#pragma unroll
-        for (int i = 0; i < kVerifyVecs; ++i)
-#pragma unroll
-          for (int e = 0; e < VE; ++e) w[i][e] = v / step == i && x % VE == e ? 0.0 : w[i][e];
-      }
-    };
+    int n_gone = num_gone;
     auto slice_sum = [&](int s, double mul) __attribute__((always_inline)) {
       double w[kVerifyVecs][VE], sum = 0.0;
-      weights(s * kSliceVecs + tid, kVerifyThreads, mul, w);
+      weights(z, q, t, mul, n_gone, s * kSliceVecs + tid, kVerifyThreads, w);
 #pragma unroll
       for (int i = 0; i < kVerifyVecs; ++i)
 #pragma unroll
@@ -517,8 +541,9 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
       return run;
     };
     all = sum_all();
-    if (all == 0.0 && c > 0.0) {  // rounding left nothing: the row's own weights
+    if (all == 0.0 && (c > 0.0 || n_gone > 0)) {  // nothing is left: the row's own weights
       mul = 0.0;
+      n_gone = 0;
       __syncthreads();
       for (int s = 0; s < slices; ++s) {
         const double m = slice_sum(s, mul);
@@ -555,7 +580,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(VerifyLaunch p) 
     double sum = 0.0, w[kVerifyVecs][VE];
     int final = -1;  // the last token of positive weight
     const int v0 = in * kSliceVecs + tid * kVerifyVecs;
-    weights(v0, 1, mul, w);
+    weights(z, q, t, mul, n_gone, v0, 1, w);
 #pragma unroll
     for (int i = 0; i < kVerifyVecs; ++i)
 #pragma unroll
