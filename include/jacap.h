@@ -521,7 +521,9 @@ typedef struct jacap_quant {
  *   acc : optional float [L][H_kv][T_total] (dense): an empty slot (an entry below zero)
  *         has no token, its codes are kept as they are.
  * Of attn live_lens is read (its other fields, num_q_heads and window are checked as by
- * jacap_attn_weights). No workspace and no flags. k, v must not overlap the codes. */
+ * jacap_attn_weights). No workspace and no flags: a sequence whose live length is below 0 or
+ * above its rows, or whose rows are not whole blocks, keeps its codes and its scales. k, v must
+ * not overlap the codes. */
 jacap_status jacap_quantize(const jacap_config* cfg, const jacap_batch* batch,
                             const jacap_attention* attn, const jacap_quant* quant, const void* k,
                             const void* v, const float* acc, void* kq, void* vq, float* scales,

@@ -113,8 +113,10 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(Geo g, Attn at, Quan
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int u = blockIdx.x / chunks, chunk = blockIdx.x - u * chunks;
   const Unit un = attention_unit(g, at, u);
-  // its rows, whether or not they hold tokens
-  const int rows = whole_blocks(g, at, un.b) ? __builtin_amdgcn_readfirstlane(decode_unit(g, u).n) : 0;
+  // Its rows, whether or not they hold tokens. A sequence whose length is not one of its rows' is
+  // left as it is: its scales would be those of no token, and what its codes stand for lost.
+  int rows = whole_blocks(g, at, un.b) ? __builtin_amdgcn_readfirstlane(decode_unit(g, u).n) : 0;
+  if (!live_ok(g, un.b, rows)) rows = 0;
   const int c0 = chunk * kQuantTokens;
   if (c0 >= rows) return;
   __shared__ uint32_t most[2][8];
