@@ -103,7 +103,6 @@ struct QuantParams {
 };
 
 // 16-token tiles of a step (a token over 131072, four layers: 162 us with 2 tiles, 176 with 4).
-template <typename T, int D, int MT>
 constexpr int kStepTiles = 2;
 
 }  // namespace
@@ -111,7 +110,8 @@ constexpr int kStepTiles = 2;
 template <typename T, int D, int MT, Mode MODE>
 __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T> params) {
   using W = Row<T, D>;
-  constexpr int NT = kStepTiles<T, D, MT>, STEP = 16 * NT, GROUP = 4 * STEP, TERMS = kTerms<T>;
+  constexpr int NT = kStepTiles, STEP = 16 * NT, GROUP = kQuantGroup, TERMS = kTerms<T>;
+  static_assert(GROUP == 4 * STEP);
   constexpr int CH = D / 16, VW = D / 64;  // channels of V per lane and token, words of codes
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, qg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -318,8 +318,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
   };
 
   // A step over the codes held, of which bit j of vis says that rows may see token j.
-  auto step = [&](uint64_t vis, int r0, float2 sc, auto fetch_k, auto fetch_v) {
-    constexpr uint64_t ALL = STEP == 64 ? ~0ull : (1ull << (STEP & 63)) - 1;
+  auto step = [&](uint32_t vis, int r0, float2 sc, auto fetch_k, auto fetch_v) {
     f32x4 z[MT][NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -328,10 +327,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
       for (int i = 0; i < MT; ++i) z[i][t] = quant_logits<TERMS, D>(kf[t], scale, qf[i]);
     }
     fetch_k();
-    if (vis != ALL) {
+    if (vis != ~0u) {
       // What no row sees takes no part, whatever it holds: its weight is 0 and so is its V,
       // since 0 times a NaN would not be.
-      const uint64_t mine = vis >> (4 * qg);  // bit 16 t + e: token 16 t + 4 q + e
+      const uint32_t mine = vis >> (4 * qg);  // bit 16 t + e: token 16 t + 4 q + e
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -527,8 +526,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
   for (int s = wave; s < dsteps; s += 4) draft_step(s * W::kStep);
   for (; r0 < t1; r0 += 4 * STEP) {
     const int next = r0 + 4 * STEP, rows = min(STEP, t1 - r0);
-    uint64_t vis = rows == 64 ? ~0ull : (1ull << rows) - 1;
-    if constexpr (HIDES) vis &= ~__ballot(a < 0.0f);
+    uint32_t vis = rows == 32 ? ~0u : (1u << rows) - 1;
+    if constexpr (HIDES) vis &= ~(uint32_t)__ballot(a < 0.0f);
     float2 then;
     step(vis, r0, sc,
          [&] {
@@ -618,10 +617,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_quant_kernel(QuantParams<T
 // The weights that rows of known lse gave the cached tokens. A workgroup lists the rows that
 // count (those of weight 0, mostly a verified tree's rejected ones, are left out before any
 // product) and holds the first of them as operands in LDS; then a stretch of a unit's
-// tokens passes them, 64 a wave at a time, the next ones' codes requested meanwhile. A lane's
-// sums are of its own row and 4 tokens a tile, the 16 rows' joined at the end; each token's
-// sum is one wave's, in the rows' order. The accepted rows of four trees over 12001 to 16450
-// tokens, 67 MB of codes and accumulators: 18 to 21 us, of which the read would take 9.
+// tokens passes them, 64 a wave at a time. A lane's sums are of its own row and 4 tokens a tile,
+// the 16 rows' joined at the end; each token's sum is one wave's, in the rows' order.
+// The codes of a wave's next 64 tokens are requested when this round's products have been
+// issued, into the same registers, so that only the joining of the rows' sums hides their
+// latency: read and products mostly take turns (63 rows over 131072 tokens, 143 MB: 39 us, of
+// which the read would take 20). In short stretches the list of rows and their operands, before
+// the first product, weigh as much: the accepted rows of four trees over 12001 to 16450
+// tokens, 67 MB of codes and accumulators, 18 to 21 us, of which the read would take 9.
 // ---------------------------------------------------------------------------
 constexpr int kSumList = 1024;          // rows listed at a time
 constexpr int kSumLds = 40 * 1024;      // of operands: three workgroups to a compute unit
@@ -835,10 +838,6 @@ hipError_t launch_attend_quant(const QuantLaunch& A, const AttendSpace& w, const
                 : attend_quant_typed<__bf16, 64>(A, w, q, kd, vd, out, lse, acc);
   return wide ? attend_quant_typed<float, 128>(A, w, q, kd, vd, out, lse, acc)
               : attend_quant_typed<float, 64>(A, w, q, kd, vd, out, lse, acc);
-}
-
-int attend_quant_group(const AttnLaunch& A, const AttendSpace& w) {
-  return 64 * (w.mt == 2 ? kStepTiles<__bf16, 128, 2> : kStepTiles<__bf16, 128, 1>);
 }
 
 // Tokens of a workgroup of the sums: an equal part for each of kQuantSumBlocks or more, in whole

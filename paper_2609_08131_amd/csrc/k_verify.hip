@@ -7,7 +7,11 @@
 // probability) of each row's token, fetched for all rows at once; then the draw passes
 // over the last row again, from L2, a slice a workgroup, and the workgroup that finishes
 // last joins the slices' sums and finds the token in one of them. Every slice's workgroup walks
-// for itself: it costs less than a launch.
+// for itself: it costs less than a launch while the walk needs no sum over the vocabulary. With
+// draft probabilities it needs one for every further sibling of a rejected row, and each of the
+// sequence's workgroups makes it for itself: 64 us a sibling at 128256 tokens (16 sequences of
+// one row and 1, 2, 4 and 8 children that are mostly rejected: 24, 97, 236 and 483 us), 18 at
+// 32000.
 //
 // (16 trees of 64 rows: 16.5 us; 31 before lanes shared a row's parts and the draw's place.)
 //

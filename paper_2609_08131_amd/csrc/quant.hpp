@@ -77,8 +77,7 @@ hipError_t launch_append(const QuantLaunch& A, const AppendArgs& p, const void* 
                          void* vq, float* scales);
 hipError_t launch_attend_quant(const QuantLaunch& A, const AttendSpace& w, const void* q, const void* kd,
                                const void* vd, void* out, float* lse, const float* acc);
-// Tokens of a group of launch_attend_quant's spans.
-int attend_quant_group(const AttnLaunch& A, const AttendSpace& w);
+constexpr int kQuantGroup = 128;  // tokens of a group of its spans
 // Adds the rows' weights, given their log-sums, to acc; status may be null.
 hipError_t launch_quant_sum(const QuantLaunch& A, const void* q, const float* lse, float* acc, uint32_t* status);
 

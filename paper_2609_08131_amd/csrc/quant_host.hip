@@ -176,7 +176,7 @@ jacap_status jacap_attend_quant(const jacap_config* cfg, const jacap_batch* batc
   }
   if (w.whole ? w.keep : attend_joins(L, w)) {
     TimedPhase tp(L.base.stream, JACAP_PHASE_ATTEND_JOIN);
-    JACAP_TRY(launch_attend_join_groups(L, w, attend_quant_group(L, w), out, ls, acc, acc_draft));
+    JACAP_TRY(launch_attend_join_groups(L, w, kQuantGroup, out, ls, acc, acc_draft));
   }
   if (sums) {
     TimedPhase tp(L.base.stream, JACAP_PHASE_ATTN_SUM);
