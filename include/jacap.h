@@ -489,9 +489,12 @@ jacap_status jacap_evict_weighted_slots(const jacap_config* cfg, const jacap_bat
  *   code  = x / scale rounded to the nearest e4m3 value, ties to even, at most 448 either
  *           way; NaN for an x that is not finite.
  *
- * The error of a value is at most 2^-4 of it, or 2^-10 scale where that is more. A scale
- * never falls: new tokens raise that of their block to what they need, and the codes it
- * holds are rounded once more in units of it (exact but for the smallest ones).
+ * The error of a value written is at most 2^-4 of it, or 2^-10 scale where that is more;
+ * above 448 2^119 (1.75 x 2^127) it is what lies above, up to 1/8 of the value. A scale never
+ * falls: new tokens raise that of their block to what they need, and the codes it holds are
+ * rounded once more in units of it, exactly but for those that become smaller than 2^-6. A raised
+ * scale is at least twice the last, so all the roundings of a value together are off by at most
+ * 2^-4 of it plus 2^-9 of the scale, however often it was raised.
  *
  * One serving loop: jacap_quantize after the prefill or its eviction; then for each step
  * jacap_attend_quant over a tree of drafted tokens, jacap_verify, jacap_attn_weights_quant
